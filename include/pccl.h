@@ -394,6 +394,133 @@ pccl_status pccl_get_setup(pccl_ctx *ctx, uint32_t *link_time_ns, uint32_t *chun
 pccl_status pccl_get_profile(pccl_ctx *ctx, double *setup_ms, double *match_ms, double *output_ms,
                              uint64_t *scan_words);
 
+/* ---- operators at the ends of a collective ---------------------------------
+ *
+ * What a step of a model puts into the collectives and does with what they
+ * deliver: packing to 4 bits (a chunk carries 4.25 bits a value instead of
+ * 16), products of packed operands, the router whose counts are the chunk
+ * counts of an expert-parallel All-to-Allv, and an expert layer for the few
+ * tokens of a decode step.
+ *
+ * They use the context for its device and its error message only: they need
+ * no topology and may be called at any time.  Arrays are DEVICE memory on the
+ * context's device unless said otherwise.  Each call queues its kernels on
+ * `hip_stream` (NULL = the default stream) and returns; it allocates nothing,
+ * copies nothing to the host and may be captured into a HIP graph.  A
+ * workspace is the caller's, 256-byte aligned, must not be shared by calls
+ * that may overlap, and needs no initial contents.  Outputs must not overlap
+ * inputs.  A row stride `ld` is counted in elements and is at least the row's
+ * length.  PCCL_EINVAL: null or misaligned arrays, bad types, strides or
+ * counts; PCCL_EUNSUPPORTED: outside the stated limits; PCCL_ENOMEM: workspace
+ * too small; PCCL_EDEVICE: a launch failed.  Extents are at most 2^31 - 1.
+ */
+typedef enum { PCCL_F32 = 0, PCCL_BF16 = 1, PCCL_F16 = 2 } pccl_dtype;
+
+/*
+ * Microscaled 4-bit values (OCP Microscaling Formats, version 1.0): blocks of
+ * 32 neighbouring values of a row share a scale.  A block's scale byte b
+ * stands for 2^(b - 127), its codes for E2M1 values (0, .5, 1, 1.5, 2, 3, 4, 6
+ * and their negatives), two to a byte, the earlier one in the low half.
+ * Stored rows end on a whole 128 values, the rest being zeros: a row of n
+ * values has ceil(n / 128) * 64 bytes of codes and ceil(n / 128) * 4 of
+ * scales.  Codes are 16-byte, scales 4-byte aligned.
+ */
+#define PCCL_MX_CODE_BYTES(n) ((((uint64_t)(n) + 127) / 128) * 64)
+#define PCCL_MX_SCALE_BYTES(n) ((((uint64_t)(n) + 127) / 128) * 4)
+
+/*
+ * Packs x (rows x cols of `dtype`, row stride ld): its rows into codes /
+ * scales, and in the same pass its columns into codes_t / scales_t (`cols`
+ * rows of `rows` values: the transpose, blocked along the rows, as the
+ * products of a training step contract over them).  Either pair may be NULL.
+ * b = max(floor(log2 a) - 2, -127) + 127 for a block with largest magnitude a,
+ * 0 for zeros; values go to the nearest, ties to the even code, and beyond 6
+ * to 6.  A block that holds a NaN or an infinity gets b = 255: all NaN.
+ */
+pccl_status pccl_mx_quantize(pccl_ctx *ctx, const void *x, pccl_dtype dtype, uint64_t rows, uint64_t cols,
+                             uint64_t ld, uint8_t *codes, uint8_t *scales, uint8_t *codes_t,
+                             uint8_t *scales_t, void *hip_stream);
+
+/* The values that codes / scales stand for, rounded to `dtype` (f32 and bf16
+ * hold every value that packing gives). */
+pccl_status pccl_mx_dequantize(pccl_ctx *ctx, const uint8_t *codes, const uint8_t *scales, uint64_t rows,
+                               uint64_t cols, void *out, pccl_dtype dtype, uint64_t ld, void *hip_stream);
+
+/* Workspace of pccl_mx_matmul; 0 where it needs none. */
+pccl_status pccl_mx_matmul_workspace(pccl_ctx *ctx, uint64_t m, uint64_t n, uint64_t k, size_t *out_bytes);
+
+/*
+ * out (m x n of `dtype`, row stride ld) = A B^T for packed A (m rows of k
+ * values) and B (n rows of k values), summed in 32 bits and rounded once.  k =
+ * 0 gives zeros.  A layer's forward product takes the packed rows of x and W,
+ * its input gradient those of dy and of W's columns, its weight gradient those
+ * of dy's and x's columns.
+ */
+pccl_status pccl_mx_matmul(pccl_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales,
+                           const uint8_t *b_codes, const uint8_t *b_scales, uint64_t m, uint64_t n,
+                           uint64_t k, void *out, pccl_dtype dtype, uint64_t ld, void *workspace,
+                           size_t workspace_bytes, void *hip_stream);
+
+/* Workspace of pccl_moe_route; 0 where it needs none. */
+pccl_status pccl_moe_route_workspace(pccl_ctx *ctx, uint64_t tokens, uint32_t experts, uint32_t topk,
+                                     size_t *out_bytes);
+
+/*
+ * The router: for each row of logits (tokens x experts of `dtype`, row stride
+ * ld) the topk largest, in descending order, ties to the lowest index.
+ *   ids[tokens][topk], weights[tokens][topk]: the picks and their softmax
+ *     weights, over the whole row or, with `normalize`, over the picks.  A
+ *     logit of minus infinity bars its expert; where fewer than topk are left
+ *     the other picks are -1 with weight 0.  A NaN counts as the largest and
+ *     makes its row's weights NaN.
+ *   token_mask: one byte a token, 0 = padding (no picks), or NULL.
+ *   counts[experts]: the picks of each expert.
+ *   order[tokens * topk]: the slots (token * topk + position) by expert, those
+ *     of one expert ascending, then -1 for every empty pick.
+ * Limits: experts <= 1024, topk <= 32, topk <= experts, tokens * topk < 2^31.
+ */
+pccl_status pccl_moe_route(pccl_ctx *ctx, const void *logits, pccl_dtype dtype, uint64_t tokens,
+                           uint32_t experts, uint64_t ld, uint32_t topk, int normalize,
+                           const uint8_t *token_mask, float *weights, int32_t *ids, int32_t *counts,
+                           int32_t *order, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * The gradient of the weights with respect to the logits, given pccl_moe_route's
+ * outputs and dweights[tokens][topk]: dlogits (tokens x experts of `dtype`, row
+ * stride ld_d).  Empty picks and their dweights do not count.  `logits` are
+ * read only without `normalize` and may be NULL with it.
+ */
+pccl_status pccl_moe_route_backward(pccl_ctx *ctx, const void *logits, pccl_dtype dtype, uint64_t tokens,
+                                    uint32_t experts, uint64_t ld, uint32_t topk, int normalize,
+                                    const uint8_t *token_mask, const float *weights, const int32_t *ids,
+                                    const float *dweights, void *dlogits, uint64_t ld_d, void *hip_stream);
+
+/* Workspace of pccl_moe_layer. */
+pccl_status pccl_moe_layer_workspace(pccl_ctx *ctx, uint32_t tokens, uint32_t experts, uint32_t topk,
+                                     uint32_t hidden, uint32_t inter, size_t *out_bytes);
+
+/*
+ * A mixture-of-experts layer for a few tokens: with l = x Wr^T and the router's
+ * picks and weights of l, y_t = sum over the picks of
+ * w Wd[e] (silu(Wg[e] x_t) * (Wu[e] x_t)).
+ *   x, y: tokens x hidden of `dtype` (PCCL_BF16 or PCCL_F16), strides ld_x, ld_y;
+ *   router: experts x hidden of `dtype`;
+ *   up: experts x (2 inter) x hidden, Wg's rows before Wu's; down: experts x
+ *     hidden x inter; of `dtype`, or packed codes with up_scales / down_scales
+ *     (both or neither NULL).  All contiguous.
+ * A token without picks (masked out) gives zeros.  Sums, the softmax and the
+ * inner values are kept in 32 bits or in two parts that hold as much; y is
+ * rounded once.  Results do not depend on the other tokens' number or picks
+ * beyond the order of 32-bit sums.
+ * Limits: tokens <= 256, experts <= 1024, topk <= 32, topk <= experts, hidden
+ * and inter <= 2^20.
+ */
+pccl_status pccl_moe_layer(pccl_ctx *ctx, const void *x, pccl_dtype dtype, uint64_t ld_x, uint32_t tokens,
+                           uint32_t experts, uint32_t topk, uint32_t hidden, uint32_t inter, int normalize,
+                           const uint8_t *token_mask, const void *router, const void *up,
+                           const uint8_t *up_scales, const void *down, const uint8_t *down_scales, void *y,
+                           uint64_t ld_y, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Message of the last failed call on this context ("" if none). */
 const char *pccl_last_error(const pccl_ctx *ctx);
 

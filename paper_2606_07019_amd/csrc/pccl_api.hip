@@ -1122,6 +1122,12 @@ bool result_alive(const pccl_ctx *c)
 
 }  // namespace
 
+// What the operators' entry points need of a context.
+namespace pccl {
+int ctx_device(const pccl_ctx *c) { return c->device; }
+void ctx_set_error(pccl_ctx *c, const char *text) { c->err = text; }
+}  // namespace pccl
+
 #define GUARD_BEGIN try {
 #define GUARD_END(ctx)                                                   \
     }                                                                    \

@@ -1,0 +1,217 @@
+"""The operators at the ends of a collective, on torch tensors.
+
+Argument marshalling over the C ABI (include/pccl.h, "operators at the ends of
+a collective"): shapes and types are checked here, the rest by the library,
+and every step runs in its HIP kernels.  Calls are queued on the current
+stream of the device; outputs and workspaces come from torch's allocator, so
+calls on different streams do not share any.
+
+    ops = Operators()
+    q = ops.quantize(x)                          # rows in 4.25 bits a value
+    y = ops.matmul(q, w, torch.bfloat16)         # q w^T
+    weights, ids, counts, order = ops.route(logits, 8)
+    y = ops.moe_layer(x, router, up, down, 8)
+"""
+
+from __future__ import annotations
+
+from typing import NamedTuple, Optional
+
+import torch
+
+from paper_2606_07019_amd import pccl as P
+
+_DTYPE = {torch.float32: P.PCCL_F32, torch.bfloat16: P.PCCL_BF16, torch.float16: P.PCCL_F16}
+
+
+class MX(NamedTuple):
+    """Packed rows: codes [..., rows, ceil(cols / 128) * 64] and scales
+    [..., rows, ceil(cols / 128) * 4] (uint8), and the rows' length."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    cols: int
+
+
+def mx_bytes(cols: int):
+    """(code bytes, scale bytes) of one packed row of `cols` values."""
+    steps = -(-cols // 128)
+    return steps * 64, steps * 4
+
+
+class Operators:
+    """A context for the operators on one device."""
+
+    def __init__(self, device: int = 0):
+        self.device = torch.device("cuda", device)
+        self._index = device
+        self.h = None
+        self.h = P.pccl_create(device, 0)
+
+    # -- checks ------------------------------------------------------------
+
+    def _matrix(self, name, x, types=_DTYPE):
+        if x.dim() != 2 or x.device != self.device or x.dtype not in types:
+            raise ValueError(f"{name}: a matrix of {', '.join(str(t) for t in types)} on {self.device} is needed, "
+                             f"got {tuple(x.shape)} {x.dtype} on {x.device}")
+        rows, cols = x.shape
+        if rows == 0 or cols == 0:
+            return rows, cols, cols
+        if cols > 1 and x.stride(1) != 1:
+            raise ValueError(f"{name}: rows must be contiguous (strides {x.stride()})")
+        return rows, cols, (x.stride(0) if rows > 1 else cols)
+
+    def _same(self, name, x, shape, dtype):
+        if tuple(x.shape) != shape or x.dtype != dtype or x.device != self.device or not x.is_contiguous():
+            raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} on {self.device} is needed, got "
+                             f"{tuple(x.shape)} {x.dtype} on {x.device}")
+        return x.data_ptr()
+
+    def _packed(self, name, q: MX, lead):
+        cb, sb = mx_bytes(q.cols)
+        return (self._same(name + " codes", q.codes, (*lead, cb), torch.uint8),
+                self._same(name + " scales", q.scales, (*lead, sb), torch.uint8))
+
+    def _mask(self, mask, tokens):
+        if mask is None:
+            return None
+        if mask.dtype == torch.bool:
+            mask = mask.view(torch.uint8)
+        return self._same("mask", mask, (tokens,), torch.uint8)
+
+    def _stream(self):
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _empty(self, shape, dtype):
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _space(self, nbytes):
+        return self._empty((nbytes,), torch.uint8) if nbytes else None
+
+    # -- microscaled 4-bit values --------------------------------------------
+
+    def _pack(self, x, rows_too, cols_too):
+        rows, cols, ld = self._matrix("x", x)
+        r = c = None
+        if rows_too:
+            cb, sb = mx_bytes(cols)
+            r = MX(self._empty((rows, cb), torch.uint8), self._empty((rows, sb), torch.uint8), cols)
+        if cols_too:
+            cb, sb = mx_bytes(rows)
+            c = MX(self._empty((cols, cb), torch.uint8), self._empty((cols, sb), torch.uint8), rows)
+        P.pccl_mx_quantize(self.h, x.data_ptr(), _DTYPE[x.dtype], rows, cols, ld,
+                           r.codes.data_ptr() if r else None, r.scales.data_ptr() if r else None,
+                           c.codes.data_ptr() if c else None, c.scales.data_ptr() if c else None, self._stream())
+        return r, c
+
+    def quantize(self, x) -> MX:
+        """x's rows, packed."""
+        return self._pack(x, True, False)[0]
+
+    def quantize_columns(self, x) -> MX:
+        """x's columns, packed (the rows of its transpose)."""
+        return self._pack(x, False, True)[1]
+
+    def quantize_both(self, x):
+        """(x's rows, x's columns), packed in one pass over x."""
+        return self._pack(x, True, True)
+
+    def dequantize(self, q: MX, dtype) -> torch.Tensor:
+        """The values that q stands for."""
+        rows = q.codes.shape[0]
+        codes, scales = self._packed("q", q, (rows,))
+        out = self._empty((rows, q.cols), dtype)
+        P.pccl_mx_dequantize(self.h, codes, scales, rows, q.cols, out.data_ptr(), _DTYPE[dtype], q.cols,
+                             self._stream())
+        return out
+
+    def matmul(self, a: MX, b: MX, dtype, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """a b^T: [rows of a, rows of b]."""
+        if a.cols != b.cols:
+            raise ValueError(f"a has rows of {a.cols} values, b of {b.cols}")
+        m, n, k = a.codes.shape[0], b.codes.shape[0], a.cols
+        ac, as_ = self._packed("a", a, (m,))
+        bc, bs = self._packed("b", b, (n,))
+        if out is None:
+            out, ld = self._empty((m, n), dtype), n
+        else:
+            rows, cols, ld = self._matrix("out", out)
+            if (rows, cols) != (m, n) or out.dtype != dtype:
+                raise ValueError(f"out: {(m, n)} of {dtype} is needed, got {(rows, cols)} of {out.dtype}")
+        nbytes = P.pccl_mx_matmul_workspace(self.h, m, n, k)
+        ws = self._space(nbytes)
+        P.pccl_mx_matmul(self.h, ac, as_, bc, bs, m, n, k, out.data_ptr(), _DTYPE[dtype], ld,
+                         ws.data_ptr() if nbytes else None, nbytes, self._stream())
+        return out
+
+    # -- router ----------------------------------------------------------------
+
+    def route(self, logits, topk: int, normalize: bool = True, mask: Optional[torch.Tensor] = None):
+        """(weights, ids, counts, order) of the topk largest logits of every row."""
+        tokens, experts, ld = self._matrix("logits", logits)
+        mp = self._mask(mask, tokens)
+        nbytes = P.pccl_moe_route_workspace(self.h, tokens, experts, topk)
+        ws = self._space(nbytes)
+        weights = self._empty((tokens, topk), torch.float32)
+        ids = self._empty((tokens, topk), torch.int32)
+        counts = self._empty((experts,), torch.int32)
+        order = self._empty((tokens * topk,), torch.int32)
+        P.pccl_moe_route(self.h, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld, topk, int(normalize),
+                         mp, weights.data_ptr(), ids.data_ptr(), counts.data_ptr(), order.data_ptr(),
+                         ws.data_ptr() if nbytes else None, nbytes, self._stream())
+        return weights, ids, counts, order
+
+    def route_backward(self, logits, weights, ids, dweights, normalize: bool = True,
+                       mask: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The gradient of route()'s weights with respect to its logits, in their type."""
+        tokens, experts, ld = self._matrix("logits", logits)
+        topk = weights.shape[1] if weights.dim() == 2 else 0
+        shape = (tokens, topk)
+        out = self._empty((tokens, experts), logits.dtype)
+        P.pccl_moe_route_backward(self.h, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld, topk,
+                                  int(normalize), self._mask(mask, tokens),
+                                  self._same("weights", weights, shape, torch.float32),
+                                  self._same("ids", ids, shape, torch.int32),
+                                  self._same("dweights", dweights, shape, torch.float32),
+                                  out.data_ptr(), experts, self._stream())
+        return out
+
+    # -- mixture-of-experts layer ------------------------------------------------
+
+    def moe_layer(self, x, router, up, down, topk: int, normalize: bool = True,
+                  mask: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """y [tokens, hidden] for x [tokens, hidden], router [experts, hidden],
+        up [experts, 2 inter, hidden] (gate rows first) and down [experts,
+        hidden, inter], the latter two of x's type or packed (MX)."""
+        tokens, hidden, ld = self._matrix("x", x, (torch.bfloat16, torch.float16))
+        experts = router.shape[0]
+        rp = self._same("router", router, (experts, hidden), x.dtype)
+        if isinstance(up, MX) != isinstance(down, MX):
+            raise ValueError("either both or neither of up and down are packed")
+        if isinstance(up, MX):
+            inter = down.cols
+            if up.cols != hidden:
+                raise ValueError(f"up: rows of {hidden} values are needed, got {up.cols}")
+            upp, ups = self._packed("up", up, (experts, 2 * inter))
+            dp, ds = self._packed("down", down, (experts, hidden))
+        else:
+            inter = down.shape[-1]
+            upp, ups = self._same("up", up, (experts, 2 * inter, hidden), x.dtype), None
+            dp, ds = self._same("down", down, (experts, hidden, inter), x.dtype), None
+        nbytes = P.pccl_moe_layer_workspace(self.h, tokens, experts, topk, hidden, inter)
+        ws = self._space(nbytes)
+        y = self._empty((tokens, hidden), x.dtype)
+        P.pccl_moe_layer(self.h, x.data_ptr(), _DTYPE[x.dtype], ld, tokens, experts, topk, hidden, inter,
+                         int(normalize), self._mask(mask, tokens), rp, upp, ups, dp, ds, y.data_ptr(), hidden,
+                         ws.data_ptr() if nbytes else None, nbytes, self._stream())
+        return y
+
+    def close(self):
+        if self.h is not None:
+            P.pccl_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

@@ -73,6 +73,16 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "pccl_get_profile": ([P, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double),
                               ctypes.POINTER(ctypes.c_double), ctypes.POINTER(U64)], I),
         "pccl_last_error": ([P], ctypes.c_char_p),
+        "pccl_mx_quantize": ([P, P, I, U64, U64, U64, P, P, P, P, P], I),
+        "pccl_mx_dequantize": ([P, P, P, U64, U64, P, I, U64, P], I),
+        "pccl_mx_matmul_workspace": ([P, U64, U64, U64, ctypes.POINTER(ctypes.c_size_t)], I),
+        "pccl_mx_matmul": ([P, P, P, P, P, U64, U64, U64, P, I, U64, P, ctypes.c_size_t, P], I),
+        "pccl_moe_route_workspace": ([P, U64, U32, U32, ctypes.POINTER(ctypes.c_size_t)], I),
+        "pccl_moe_route": ([P, P, I, U64, U32, U64, U32, I, P, P, P, P, P, P, ctypes.c_size_t, P], I),
+        "pccl_moe_route_backward": ([P, P, I, U64, U32, U64, U32, I, P, P, P, P, P, U64, P], I),
+        "pccl_moe_layer_workspace": ([P, U32, U32, U32, U32, U32, ctypes.POINTER(ctypes.c_size_t)], I),
+        "pccl_moe_layer": ([P, P, I, U64, U32, U32, U32, U32, U32, I, P, P, P, P, P, P, P, U64, P,
+                            ctypes.c_size_t, P], I),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -256,6 +266,66 @@ def pccl_get_setup(h, n_links: int, n_chunks: int):
     rank = np.zeros(n_chunks, np.uint32)
     _check(h, load_library().pccl_get_setup(h, _np_ptr(T), _np_ptr(src), _np_ptr(dist), _np_ptr(rank)))
     return T, src, dist, rank
+
+
+# ---- operators at the ends of a collective: addresses of device memory ---------
+# (paper_2606_07019_amd.operators takes tensors)
+
+PCCL_F32, PCCL_BF16, PCCL_F16 = 0, 1, 2
+
+
+def pccl_mx_quantize(h, x, dtype, rows, cols, ld, codes=None, scales=None, codes_t=None, scales_t=None,
+                     stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_mx_quantize(h, x, dtype, rows, cols, ld, codes, scales, codes_t, scales_t,
+                                              stream_ptr or None))
+
+
+def pccl_mx_dequantize(h, codes, scales, rows, cols, out, dtype, ld, stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_mx_dequantize(h, codes, scales, rows, cols, out, dtype, ld, stream_ptr or None))
+
+
+def pccl_mx_matmul_workspace(h, m, n, k) -> int:
+    out = ctypes.c_size_t()
+    _check(h, load_library().pccl_mx_matmul_workspace(h, m, n, k, ctypes.byref(out)))
+    return int(out.value)
+
+
+def pccl_mx_matmul(h, a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld, workspace=None, nbytes=0,
+                   stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_mx_matmul(h, a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld,
+                                            workspace, nbytes, stream_ptr or None))
+
+
+def pccl_moe_route_workspace(h, tokens, experts, topk) -> int:
+    out = ctypes.c_size_t()
+    _check(h, load_library().pccl_moe_route_workspace(h, tokens, experts, topk, ctypes.byref(out)))
+    return int(out.value)
+
+
+def pccl_moe_route(h, logits, dtype, tokens, experts, ld, topk, normalize, token_mask, weights, ids, counts, order,
+                   workspace=None, nbytes=0, stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_moe_route(h, logits, dtype, tokens, experts, ld, topk, normalize, token_mask,
+                                            weights, ids, counts, order, workspace, nbytes, stream_ptr or None))
+
+
+def pccl_moe_route_backward(h, logits, dtype, tokens, experts, ld, topk, normalize, token_mask, weights, ids,
+                            dweights, dlogits, ld_d, stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_moe_route_backward(h, logits, dtype, tokens, experts, ld, topk, normalize,
+                                                     token_mask, weights, ids, dweights, dlogits, ld_d,
+                                                     stream_ptr or None))
+
+
+def pccl_moe_layer_workspace(h, tokens, experts, topk, hidden, inter) -> int:
+    out = ctypes.c_size_t()
+    _check(h, load_library().pccl_moe_layer_workspace(h, tokens, experts, topk, hidden, inter, ctypes.byref(out)))
+    return int(out.value)
+
+
+def pccl_moe_layer(h, x, dtype, ld_x, tokens, experts, topk, hidden, inter, normalize, token_mask, router, up,
+                   up_scales, down, down_scales, y, ld_y, workspace=None, nbytes=0, stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_moe_layer(h, x, dtype, ld_x, tokens, experts, topk, hidden, inter, normalize,
+                                            token_mask, router, up, up_scales, down, down_scales, y, ld_y,
+                                            workspace, nbytes, stream_ptr or None))
 
 
 # ---- convenience wrapper (marshalling of a whole workload) --------------------
