@@ -513,7 +513,7 @@ pccl_status pccl_moe_layer_workspace(pccl_ctx *ctx, uint32_t tokens, uint32_t ex
  * rounded once.  Results do not depend on the other tokens' number or picks
  * beyond the order of 32-bit sums.
  * Limits: tokens <= 256, experts <= 1024, topk <= 32, topk <= experts, hidden
- * and inter <= 2^20.
+ * and inter <= 2^20, hidden * inter <= 2^29.
  */
 pccl_status pccl_moe_layer(pccl_ctx *ctx, const void *x, pccl_dtype dtype, uint64_t ld_x, uint32_t tokens,
                            uint32_t experts, uint32_t topk, uint32_t hidden, uint32_t inter, int normalize,

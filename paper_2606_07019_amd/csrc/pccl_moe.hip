@@ -7,39 +7,47 @@
 // columns, so the layer is bound by that reading; the matrix units are used
 // because they take 16 tokens at the price of one.  Weight rows are the first
 // operand of the 16x16x32 products (lane l: row l % 16, eight values of k per
-// product), the expert's tokens the second.  Weights go from memory to
-// registers, each used once there.
+// product), the expert's tokens the second.  Neighbouring lanes thus need
+// neighbouring rows, while memory wants them along a row (a compute unit's
+// port takes one 64-byte piece a cycle: read in the operands' order, 1 KiB
+// took 64 cycles and that bounded the kernels).  So a wave reads weights along
+// their rows into registers, several blocks ahead (registers hold more of what
+// is on its way than LDS could), and turns a block round through 4 KiB of LDS
+// of its own when it multiplies it.
 #include "pccl_topk.h"
 
 namespace pccl {
 namespace {
 
-constexpr uint32_t STEP = 128;      // values of k a wave takes at a time: four products
-constexpr int WAVES = 4;
-constexpr int TILES = 4;            // tiles of 16 tokens that share one reading of the weights
+constexpr uint32_t STEP = 128;      // rows of inner values are padded to whole steps of 128
+constexpr int WAVES = 4;            // waves of a workgroup that share out k
+constexpr int PICK_WAVES = 16;
+constexpr uint32_t NO_PLACE = 0xFFFFFFFFu;
+constexpr uint32_t MAX_SPLITS = 8;  // parts of the router's product over hidden, summed up by the picking lanes
 
 // What the kernels of one call hand on, carved from the workspace.
 struct MoeSpace {
-    float *part_logits;   // [splits][tokens][experts]
-    int32_t *ids;         // [tokens][topk]
-    float *weights;       // [tokens][topk]
-    int32_t *place;       // [tokens][topk]: the slot's place in expert order, -1 for none
+    float *part_logits;   // [splits][tokens][experts padded to 16]
     uint32_t *active;     // [0]: experts in use; then the experts
     uint32_t *first;      // [experts in use + 1]: where each one's places start
-    uint32_t *slots;      // [places]: token of each place
-    uint16_t *hi, *lo;    // [places][inner size padded to a step]: the inner values, in two parts
-    float *outs;          // [places][hidden]
+    uint32_t *slots;      // [places]: token of each place, in expert order
+    float *shares;        // [places]: its weight
+    uint32_t *place;      // [tokens][topk]: the slot's place, NO_PLACE for an empty pick
+    uint16_t *hi, *lo;    // the inner values, in two parts: [tiles of 16 places][products][lane][8], as
+                          // the products' second operands have them
+    float *outs;          // [places][hidden]: the experts' outputs, weighted
     uint64_t inner;       // padded inner size
-    uint32_t splits;
+    uint32_t splits, row; // parts of the logits, and the length of their rows
 };
 
-// Workgroups that share the router's product over hidden: enough for the
-// chip's compute units to have one each.
-__host__ inline uint32_t logit_splits(uint32_t experts, uint32_t hidden)
+// Workgroups that share the router's product over hidden, so that about 128
+// take part.
+__host__ inline uint32_t logit_splits(uint32_t tokens, uint32_t experts, uint32_t hidden)
 {
-    const uint32_t tiles = (experts + 15) / 16, steps = (hidden + STEP - 1) / STEP;
-    const uint32_t want = (128 + tiles - 1) / tiles;
-    return want < steps ? want : steps;
+    const uint32_t tiles = (experts + 15) / 16 * ((tokens + 15) / 16), most = (hidden + STEP - 1) / STEP;
+    uint32_t want = (128 + tiles - 1) / tiles;
+    if (want > MAX_SPLITS) want = MAX_SPLITS;
+    return want < most ? want : most;
 }
 
 __host__ inline size_t carve(MoeSpace &m, char *base, uint32_t tokens, uint32_t experts, uint32_t topk, uint32_t hidden, uint32_t inter)
@@ -51,17 +59,18 @@ __host__ inline size_t carve(MoeSpace &m, char *base, uint32_t tokens, uint32_t 
         return p;
     };
     const uint64_t places = (uint64_t)tokens * topk;
-    m.splits = logit_splits(experts, hidden);
+    m.splits = logit_splits(tokens, experts, hidden);
     m.inner = (inter + STEP - 1) / STEP * (uint64_t)STEP;
-    m.part_logits = (float *)take((size_t)m.splits * tokens * experts * 4);
-    m.ids = (int32_t *)take(places * 4);
-    m.weights = (float *)take(places * 4);
-    m.place = (int32_t *)take(places * 4);
+    m.row = (experts + 15) / 16 * 16;
+    m.part_logits = (float *)take((size_t)m.splits * tokens * m.row * 4);
     m.active = (uint32_t *)take((experts + 1ull) * 4);
     m.first = (uint32_t *)take((experts + 1ull) * 4);
     m.slots = (uint32_t *)take(places * 4);
-    m.hi = (uint16_t *)take(places * m.inner * 2);
-    m.lo = (uint16_t *)take(places * m.inner * 2);
+    m.shares = (float *)take(places * 4);
+    m.place = (uint32_t *)take(places * 4);
+    const uint64_t tiles = places / 16 + (places < experts ? places : experts) + 1;
+    m.hi = (uint16_t *)take(tiles * 16 * m.inner * 2);
+    m.lo = (uint16_t *)take(tiles * 16 * m.inner * 2);
     m.outs = (float *)take(places * hidden * 4);
     return off;
 }
@@ -100,45 +109,176 @@ __device__ inline u32x4 row8(const uint16_t *row, uint32_t k, uint32_t end)
     return v;
 }
 
-// One step of weights: what a lane holds of a row, and its four first
-// operands.  16-bit rows: product i takes values 32 i + 8 (l / 16) ... + 7 of
-// the step; microscaled rows: a lane's 16 bytes are one block, product i takes
-// its values 8 i ... + 7 (both operands count k alike, so the order is free).
-template <class T, bool VEC>
+// Weight rows as a wave reads them: blocks of M tiles of 16 rows by VALUES of
+// k.  begin() takes a tile's rows, read() starts a block's reads (a lane takes
+// chunks of 16 bytes, neighbours along a row), turn() writes them to LDS, and
+// operand() gives the lane's eight values of a product there: chunk c of row r
+// stands where the 16 lanes that read one chunk of 16 rows meet every bank
+// once.
+//
+// 16-bit rows: 128 bytes and two products a block; product i takes values 32 i
+// + 8 (l / 16) ... + 7.  Microscaled rows: 64 bytes, four products; a lane's
+// chunk is one group of 32 values with its scale, and product j takes its
+// values 8 j ... + 7 (both operands count k alike, so the order is free).
+
+// A matrix of one expert: rows of `len` bytes, 32-bit offsets from `base`.
+struct Rows {
+    const char *base;
+    const uint8_t *scales;
+    uint32_t rows, len, slen;
+};
+
+template <class T, int M>
 struct Plain {
     typedef T C;                         // the products' type
-    static constexpr bool MX = false;
-    u32x4 v[4];
-    __device__ void load(const uint16_t *row, const uint8_t *, uint32_t step, uint32_t g, uint32_t end)
+    static constexpr uint32_t PRODUCTS = 2, VALUES = 64, LDS = M * 2048;
+    struct Block {
+        u32x4 v[2 * M];
+    };
+    uint32_t off[2 * M], chunk[2], len;
+
+    // tile t of M rows; `apart`: rows between the M sub-tiles
+    __device__ void begin(const Rows &w, const uint32_t (&row)[M])
+    {
+        const uint32_t lane = threadIdx.x & 63u;
+        len = w.len;
+#pragma unroll
+        for (uint32_t q = 0; q < 2; q++) {
+            chunk[q] = lane % 8 * 16u;
+#pragma unroll
+            for (int i = 0; i < M; i++) {
+                const uint32_t r = row[i] + q * 8u + lane / 8;
+                off[2 * i + q] = (r < w.rows ? r : w.rows - 1) * w.len;
+            }
+        }
+    }
+    __device__ void read(Block &b, const Rows &w, uint32_t block, bool there) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; i++) v[i] = row8<VEC>(row, step * STEP + i * 32u + g * 8u, end);
+        for (int j = 0; j < 2 * M; j++) {   // chunks past the row's end are read from its start and not used
+            const uint32_t at = block * 128u + chunk[j % 2], from = off[j] + (at < len ? at : 0u);
+            b.v[j] = *reinterpret_cast<const u32x4 *>(w.base + (there ? from : 0u));
+        }
     }
-    __device__ u32x4 operand(int i) const { return v[i]; }
-    static __device__ uint32_t at(uint32_t step, uint32_t g, int i) { return step * STEP + i * 32u + g * 8u; }
+    __device__ void turn(const Block &b, uint8_t *lds, uint32_t block) const
+    {
+        const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+        for (int j = 0; j < 2 * M; j++) {
+            const uint32_t r = j % 2 * 8u + lane / 8;
+            u32x4 v = b.v[j];
+            if (block * 128u + chunk[j % 2] >= len) v = u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4 *>(lds + j / 2 * 2048u + r * 128u + ((lane % 8) ^ (r / 2)) * 16u) = v;
+        }
+    }
+    __device__ void operands(const uint8_t *lds, int i, uint32_t r, uint32_t g, u32x4 (&v)[PRODUCTS]) const
+    {
+#pragma unroll
+        for (uint32_t p = 0; p < PRODUCTS; p++)
+            v[p] = *reinterpret_cast<const u32x4 *>(lds + i * 2048u + r * 128u + (((p * 4u + g) ^ (r / 2)) * 16u));
+    }
+    static __device__ uint32_t at(uint32_t block, uint32_t g, uint32_t p) { return block * VALUES + p * 32u + g * 8u; }
+    // the product and lane group that take value k, for its place among the second operands
+    static __device__ void place(uint32_t k, uint32_t &product, uint32_t &g)
+    {
+        product = k / 32;
+        g = k % 32 / 8;
+    }
 };
+
+// The same values where rows do not start on 16 bytes: read one by one, in the operands' order.
+template <class T, int M>
+struct Loose {
+    typedef T C;
+    static constexpr uint32_t PRODUCTS = 2, VALUES = 64, LDS = M * 2048;
+    struct Block {
+        u32x4 v[2 * M];
+    };
+    uint32_t off[M];
+    __device__ void begin(const Rows &w, const uint32_t (&row)[M])
+    {
+#pragma unroll
+        for (int i = 0; i < M; i++) {
+            const uint32_t r = row[i] + (threadIdx.x & 15u);
+            off[i] = (r < w.rows ? r : w.rows - 1) * w.len;
+        }
+    }
+    __device__ void read(Block &b, const Rows &w, uint32_t block, bool there) const
+    {
+        const uint32_t g = (threadIdx.x & 63u) >> 4;
+        if (!there) return;
+#pragma unroll
+        for (int i = 0; i < M; i++)
+#pragma unroll
+            for (uint32_t p = 0; p < 2; p++)
+                b.v[2 * i + p] = row8<false>(reinterpret_cast<const uint16_t *>(w.base + off[i]), at(block, g, p), w.len / 2);
+    }
+    __device__ void turn(const Block &b, uint8_t *lds, uint32_t) const
+    {
+#pragma unroll
+        for (int j = 0; j < 2 * M; j++) reinterpret_cast<u32x4 *>(lds)[j * 64 + (threadIdx.x & 63u)] = b.v[j];
+    }
+    __device__ void operands(const uint8_t *lds, int i, uint32_t, uint32_t, u32x4 (&v)[PRODUCTS]) const
+    {
+#pragma unroll
+        for (uint32_t p = 0; p < 2; p++) v[p] = reinterpret_cast<const u32x4 *>(lds)[(2 * i + p) * 64 + (threadIdx.x & 63u)];
+    }
+    static __device__ uint32_t at(uint32_t block, uint32_t g, uint32_t p) { return Plain<T, M>::at(block, g, p); }
+    static __device__ void place(uint32_t k, uint32_t &product, uint32_t &g) { Plain<T, M>::place(k, product, g); }
+};
+
+template <int M>
 struct Micro {
     typedef __bf16 C;                    // holds every microscaled value exactly
-    static constexpr bool MX = true;
-    u32x4 v;
-    uint32_t byte;
-    __device__ void load(const uint16_t *row, const uint8_t *scales, uint32_t step, uint32_t g, uint32_t)
+    static constexpr uint32_t PRODUCTS = 4, VALUES = 128, LDS = M * 1024 + 256;
+    static_assert(M <= 4, "a lane reads one word of scales a block");
+    struct Block {
+        u32x4 v[M];
+        uint32_t s;
+    };
+    uint32_t off[M], soff;
+    __device__ void begin(const Rows &w, const uint32_t (&row)[M])
     {
-        v = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint8_t *>(row) + step * 64u + g * 16u);
-        byte = scales[step * 4u + g];
+        const uint32_t lane = threadIdx.x & 63u;
+        soff = 0;
+#pragma unroll
+        for (int i = 0; i < M; i++) {
+            const uint32_t r = row[i] + lane / 4, q = row[i] + lane % 16;
+            off[i] = (r < w.rows ? r : w.rows - 1) * w.len + lane % 4 * 16u;
+            if (lane / 16 == (uint32_t)i) soff = (q < w.rows ? q : w.rows - 1) * w.slen;
+        }
     }
-    __device__ u32x4 operand(int i) const
+    __device__ void read(Block &b, const Rows &w, uint32_t block, bool there) const
     {
-        const float s = mx_scale(byte);
-        const uint32_t c = v[i];
-        u32x4 r;
-        r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
-        r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
-        r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
-        r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
-        return r;
+#pragma unroll
+        for (int i = 0; i < M; i++) b.v[i] = *reinterpret_cast<const u32x4 *>(w.base + (there ? off[i] + block * 64u : 0u));
+        b.s = *reinterpret_cast<const uint32_t *>(w.scales + (there ? soff + block * 4u : 0u));
     }
-    static __device__ uint32_t at(uint32_t step, uint32_t g, int i) { return step * STEP + g * 32u + i * 8u; }
+    __device__ void turn(const Block &b, uint8_t *lds, uint32_t) const
+    {
+        const uint32_t lane = threadIdx.x & 63u, r = lane / 4;
+#pragma unroll
+        for (int i = 0; i < M; i++) *reinterpret_cast<u32x4 *>(lds + i * 1024u + r * 64u + ((lane % 4) ^ (r / 4)) * 16u) = b.v[i];
+        reinterpret_cast<uint32_t *>(lds + M * 1024u)[lane] = b.s;
+    }
+    __device__ void operands(const uint8_t *lds, int i, uint32_t r, uint32_t g, u32x4 (&v)[PRODUCTS]) const
+    {
+        const u32x4 c = *reinterpret_cast<const u32x4 *>(lds + i * 1024u + r * 64u + ((g ^ (r / 4)) * 16u));
+        const float f = mx_scale(lds[M * 1024u + (i * 16u + r) * 4u + g]);
+#pragma unroll
+        for (uint32_t p = 0; p < PRODUCTS; p++) {
+            v[p].x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[p], f, 0));
+            v[p].y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[p], f, 1));
+            v[p].z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[p], f, 2));
+            v[p].w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[p], f, 3));
+        }
+    }
+    static __device__ uint32_t at(uint32_t block, uint32_t g, uint32_t p) { return block * VALUES + g * 32u + p * 8u; }
+    static __device__ void place(uint32_t k, uint32_t &product, uint32_t &g)
+    {
+        product = k / 128 * 4 + k % 32 / 8;
+        g = k % 128 / 32;
+    }
 };
 
 // A 32-bit value in two parts of the products' type: v = hi HI + lo LO.  The
@@ -165,312 +305,567 @@ __device__ inline void split(float v, uint16_t &hi, uint16_t &lo)
     lo = __builtin_bit_cast(uint16_t, l);
 }
 
+// A value that all lanes of a wave have alike, kept as one.
+__device__ inline uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
 // ---- the router's product -------------------------------------------------------
+
+// Sums of products `first`, `first` + `by`, ... of 32 values of k: 16 experts
+// from e0 on (rows) by 16 tokens from t0 on.
+template <class T, bool VEC>
+__device__ inline f32x4 logit_tile(const MoeArgs &a, uint32_t e0, uint32_t t0, uint32_t first, uint32_t by, uint32_t r, uint32_t g)
+{
+    const uint32_t e = e0 + r < a.experts ? e0 + r : a.experts - 1;
+    const uint32_t t = t0 + r < a.tokens ? t0 + r : a.tokens - 1;
+    const uint16_t *wrow = static_cast<const uint16_t *>(a.router) + (uint64_t)e * a.hidden;
+    const uint16_t *xrow = static_cast<const uint16_t *>(a.x) + (uint64_t)t * a.ld_x;
+    const uint32_t products = (a.hidden + 31) / 32;
+    f32x4 acc = {};
+    uint32_t p = first;
+    constexpr int U = VEC ? 8 : 2;   // so many at a time: their reads are under way together
+    for (; p + (U - 1) * by < products; p += U * by) {
+        u32x4 w[U], x[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            w[u] = row8<VEC>(wrow, (p + u * by) * 32u + g * 8u, a.hidden);
+            x[u] = row8<VEC>(xrow, (p + u * by) * 32u + g * 8u, a.hidden);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) acc = Frag<T>::mul(w[u], x[u], acc);
+    }
+    for (; p < products; p += by) {
+        const uint32_t k = p * 32u + g * 8u;
+        acc = Frag<T>::mul(row8<VEC>(wrow, k, a.hidden), row8<VEC>(xrow, k, a.hidden), acc);
+    }
+    return acc;
+}
 
 // A workgroup: 16 experts, 16 tokens, one part of hidden, shared out over its waves.
 template <class T, bool VEC>
 __global__ __launch_bounds__(64 * WAVES) void k_moe_logits(MoeArgs a, MoeSpace m)
 {
     __shared__ f32x4 sums[WAVES][64];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane & 15u, g = lane >> 4;
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), r = lane & 15u, g = lane >> 4;
     const uint32_t e0 = blockIdx.x * 16u, t0 = blockIdx.z * 16u;
-    const uint32_t e = e0 + r < a.experts ? e0 + r : a.experts - 1;
-    const uint32_t t = t0 + r < a.tokens ? t0 + r : a.tokens - 1;
-    const uint16_t *wrow = static_cast<const uint16_t *>(a.router) + (uint64_t)e * a.hidden;
-    const uint16_t *xrow = static_cast<const uint16_t *>(a.x) + (uint64_t)t * a.ld_x;
-    const uint32_t products = (a.hidden + 31) / 32;
-    const uint32_t parts = m.splits * WAVES, mine = blockIdx.y * WAVES + wave;
-    f32x4 acc = {};
-    for (uint32_t p = mine; p < products; p += parts) {
-        const uint32_t k = p * 32u + g * 8u;
-        acc = Frag<T>::mul(row8<VEC>(wrow, k, a.hidden), row8<VEC>(xrow, k, a.hidden), acc);
-    }
-    sums[wave][lane] = acc;
+    sums[wave][lane] = logit_tile<T, VEC>(a, e0, t0, blockIdx.y * WAVES + wave, m.splits * WAVES, r, g);
     __syncthreads();
     if (wave) return;
     f32x4 v = sums[0][lane];
 #pragma unroll
     for (int w = 1; w < WAVES; w++) v += sums[w][lane];
-    if (t0 + r < a.tokens) {
-        float *out = m.part_logits + ((uint64_t)blockIdx.y * a.tokens + t0 + r) * a.experts;
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-            if (e0 + g * 4 + i < a.experts) out[e0 + g * 4 + i] = v[i];
-    }
+    if (t0 + r < a.tokens)
+        *reinterpret_cast<f32x4 *>(m.part_logits + ((uint64_t)blockIdx.y * a.tokens + t0 + r) * m.row + e0 + g * 4u) = v;
 }
 
 // ---- the picks --------------------------------------------------------------------
 
-constexpr int PICK_WAVES = 16;
-
-// One workgroup: every token's picks, then the experts in use with their
-// tokens.  One bit for every (expert, token) as in the router.
-template <int VPL>
+// One workgroup: every token's picks (16 or 64 lanes a row, as in the router),
+// then the experts in use with their tokens, by one bit for every (expert,
+// token).  All of it stays in LDS; bound by the latency of its few steps.
+template <int LANES, int V>
 __global__ __launch_bounds__(64 * PICK_WAVES) void k_moe_pick(MoeArgs a, MoeSpace m)
 {
-    constexpr int SETS = MOE_MAX_TOKENS / 64;
-    __shared__ uint64_t rows[SETS][64 * VPL];
-    __shared__ uint32_t base[64 * VPL], sums[PICK_WAVES];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    for (uint32_t i = threadIdx.x; i < SETS * 64 * VPL; i += 64 * PICK_WAVES) (&rows[0][0])[i] = 0;
+    constexpr int HELD = picks_held<LANES>(), PER = 64 / LANES;
+    extern __shared__ __align__(16) unsigned long long rows[];   // [sets of 64 tokens][experts], then the rest
+    __shared__ uint32_t sums[PICK_WAVES];
+    const uint32_t sets = (a.tokens + 63) / 64, slots = a.tokens * a.topk;
+    uint32_t *base = reinterpret_cast<uint32_t *>(rows + sets * a.experts);
+    int32_t *ids = reinterpret_cast<int32_t *>(base + a.experts);
+    float *weights = reinterpret_cast<float *>(ids + slots);
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), sub = lane % LANES;
+    for (uint32_t i = threadIdx.x; i < sets * a.experts; i += 64 * PICK_WAVES) rows[i] = 0;
     __syncthreads();
-    for (uint32_t t = wave; t < a.tokens; t += PICK_WAVES) {
-        const bool there = !a.mask || a.mask[t];
-        uint32_t key[VPL];
+    for (uint32_t t0 = wave * PER; t0 < a.tokens; t0 += PICK_WAVES * PER) {
+        const uint32_t t = t0 + lane / LANES, row = t < a.tokens ? t : a.tokens - 1;
+        f32x4 v[V / 4] = {};
+        if (sub * V < m.row) {
+            const float *q = m.part_logits + (uint64_t)row * m.row + sub * V;
+            const uint64_t by = (uint64_t)a.tokens * m.row;
 #pragma unroll
-        for (int i = 0; i < VPL; i++) {
-            const uint32_t e = lane * VPL + i;
-            key[i] = 0;
-            if (there && e < a.experts) {
-                float v = 0.f;
-                for (uint32_t s = 0; s < m.splits; s++) v += m.part_logits[((uint64_t)s * a.tokens + t) * a.experts + e];
-                key[i] = key_of(v);
-            }
+            for (uint32_t s = 0; s < MAX_SPLITS; s++)
+                if (s < m.splits) {
+#pragma unroll
+                    for (int i = 0; i < V / 4; i++)
+                        if (sub * V + i * 4 < m.row) v[i] += *reinterpret_cast<const f32x4 *>(q + s * by + i * 4);
+                }
         }
-        int32_t id;
-        float w;
-        topk_row<VPL>(key, a.topk, a.normalize, lane, id, w);
-        if (lane < a.topk) {
-            m.ids[t * a.topk + lane] = id;
-            m.weights[t * a.topk + lane] = w;
-            if (id >= 0) atomicOr((unsigned long long *)&rows[t / 64][id], 1ull << (t % 64));   // LDS; bits of a set
+        const bool there = !a.mask || a.mask[row];
+        uint32_t key[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) key[i] = there && sub * V + i < a.experts ? Key<float>::of(v[i / 4][i % 4], 0) : 0u;
+        int32_t id[HELD];
+        float w[HELD];
+        topk_row<float, LANES, V>(key, a.topk, a.normalize, sub, id, w);
+#pragma unroll
+        for (int h = 0; h < HELD; h++) {
+            const uint32_t j = sub + 16u * h;
+            if (t >= a.tokens || j >= a.topk) continue;
+            ids[t * a.topk + j] = id[h];
+            weights[t * a.topk + j] = w[h];
+            if (id[h] >= 0) atomicOr(&rows[t / 64 * a.experts + id[h]], 1ull << (t % 64));   // LDS; bits of a set
         }
     }
-    __threadfence_block();
     __syncthreads();
-    // threads take experts in order (all of them at most 1,024 = the workgroup)
+    // threads take experts in order (all of them at most 1,024 = the workgroup);
+    // both scans at once: experts in use above bit 16, their places below
     const uint32_t e = threadIdx.x;
     uint32_t c = 0;
-    if (e < a.experts) {
-#pragma unroll
-        for (int q = 0; q < SETS; q++) c += (uint32_t)__popcll(rows[q][e]);
-    }
-    uint32_t places, used;
-    const uint32_t at = block_scan<PICK_WAVES>(c, sums, places);
-    const uint32_t nth = block_scan<PICK_WAVES>(c ? 1u : 0u, sums, used);
-    if (e < a.experts) base[e] = at;
+    if (e < a.experts)
+        for (uint32_t q = 0; q < sets; q++) c += (uint32_t)__popcll(rows[q * a.experts + e]);
+    uint32_t all;
+    const uint32_t at = block_scan<PICK_WAVES>(c | (c ? 1u << 16 : 0u), sums, all);
+    if (e < a.experts) base[e] = at & 0xFFFFu;
     if (c) {
-        m.active[1 + nth] = e;
-        m.first[nth] = at;
+        m.active[1 + (at >> 16)] = e;
+        m.first[at >> 16] = at & 0xFFFFu;
     }
     if (threadIdx.x == 0) {
-        m.active[0] = used;
-        m.first[used] = places;
+        m.active[0] = all >> 16;
+        m.first[all >> 16] = all & 0xFFFFu;
     }
     __syncthreads();
-    for (uint32_t s = threadIdx.x; s < a.tokens * a.topk; s += 64 * PICK_WAVES) {
-        const int32_t id = m.ids[s];
-        const uint32_t t = s / a.topk;
-        int32_t p = -1;
-        if (id >= 0) {
-            uint32_t below = 0;
-            for (uint32_t q = 0; q < t / 64; q++) below += (uint32_t)__popcll(rows[q][id]);
-            below += (uint32_t)__popcll(rows[t / 64][id] & ((1ull << (t % 64)) - 1ull));
-            p = (int32_t)(base[id] + below);
-            m.slots[p] = t;
+    for (uint32_t s = threadIdx.x; s < slots; s += 64 * PICK_WAVES) {
+        const int32_t id = ids[s];
+        if (id < 0) {
+            m.place[s] = NO_PLACE;
+            continue;
         }
-        m.place[s] = p;
+        const uint32_t t = s / a.topk;
+        uint32_t place = base[id];
+        for (uint32_t q = 0; q < t / 64; q++) place += (uint32_t)__popcll(rows[q * a.experts + id]);
+        place += (uint32_t)__popcll(rows[t / 64 * a.experts + id] & ((1ull << (t % 64)) - 1ull));
+        m.slots[place] = t;
+        m.shares[place] = weights[s];
+        m.place[s] = place;
     }
 }
+static_assert(MOE_MAX_TOKENS * ROUTE_MAX_TOPK < 1u << 16, "places fit 16 bits of the scan");
 
 // ---- gate and up ---------------------------------------------------------------------
 
-// Sums of one step's four products for the rows of `w` and NT tiles of tokens.
-template <class T, class W, bool VEC, int NT>
-__device__ inline void step_x(const W &w, const uint16_t *const (&x)[NT], uint32_t step, uint32_t g, uint32_t end, f32x4 (&acc)[NT])
+// Both kernels below: tiles of M x 16 rows of one expert in use, for all its
+// tokens, NT tiles of 16 at a time.  Where many experts may be in use a wave
+// has tiles of its own; where few are, the four waves of a workgroup SHARE a
+// tile's k and join their sums in LDS in their order.
+struct Walk {
+    uint32_t tile, tiles, by;   // this wave's tiles
+    uint32_t b0, b1;            // this wave's blocks of k
+    uint32_t p0, p1;            // the expert's places, taken 16 NT at a time
+};
+struct At {
+    uint32_t tile, b, p;
+};
+
+template <bool SHARE>
+__device__ inline Walk share_out(const MoeSpace &m, uint32_t wave, uint32_t tiles, uint32_t blocks)
+{
+    Walk w;
+    const uint32_t per = SHARE ? (blocks + WAVES - 1) / WAVES : blocks;
+    w.tile = SHARE ? blockIdx.x : blockIdx.x * WAVES + wave;
+    w.tiles = tiles;
+    w.by = SHARE ? gridDim.x : gridDim.x * WAVES;
+    w.b0 = SHARE ? wave * per : 0u;
+    w.b1 = w.b0 + per < blocks ? w.b0 + per : blocks;
+    w.p0 = m.first[blockIdx.y];
+    w.p1 = m.first[blockIdx.y + 1];
+    return w;
+}
+
+template <int I>
+struct Index {
+    static constexpr int value = I;
+};
+
+// Runs a wave through its tiles, tokens and blocks with DEPTH blocks held or
+// on their way: read(d, at, there) starts the reads of what block `at` takes
+// into buffer d, multiply(d, at, n) makes its products, join(at, n) ends a
+// tile.  Past the end (not `there`) read makes as many reads of nothing in
+// particular: their number must not depend on a branch, or the compiler has to
+// wait for all of them where a block of several under way is used.
+template <int NT, int DEPTH, class Read, class Multiply, class Join>
+__device__ inline void walk(const Walk &w, Read read, Multiply multiply, Join join)
+{
+    auto next = [&](At at) {
+        if (++at.b < w.b1) return at;
+        at.b = w.b0;
+        at.p += 16 * NT;
+        if (at.p < w.p1) return at;
+        at.p = w.p0;
+        at.tile += w.by;
+        return at;
+    };
+    auto count = [&](const At &at) { return w.p1 - at.p < 16 * NT ? w.p1 - at.p : 16 * NT; };
+    At q[DEPTH];
+    q[0] = At{w.tile, w.b0, w.p0};
+    if (w.b0 >= w.b1) {   // no blocks for this wave: it only joins
+        for (At at = q[0]; at.tile < w.tiles; at = next(at)) join(at, count(at));
+        return;
+    }
+    auto start = [&](auto at) {
+        constexpr int d = decltype(at)::value;
+        if constexpr (d < DEPTH) {
+            if constexpr (d > 0) q[d] = next(q[d - 1]);
+            read(d, q[d], q[d].tile < w.tiles);
+        }
+    };
+    // a buffer's block, then the reads of the one DEPTH further on; false at the end
+    auto turn = [&](auto at) {
+        constexpr int d = decltype(at)::value;
+        if constexpr (d < DEPTH) {
+            if (q[d].tile >= w.tiles) return false;
+            multiply(d, q[d], count(q[d]));
+            if (q[d].b + 1 == w.b1) join(q[d], count(q[d]));
+            q[d] = next(q[(d + DEPTH - 1) % DEPTH]);
+            read(d, q[d], q[d].tile < w.tiles);
+        }
+        return true;
+    };
+    static_assert(DEPTH <= 4, "buffers written out below");
+    start(Index<0>{});
+    start(Index<1>{});
+    start(Index<2>{});
+    start(Index<3>{});
+    while (turn(Index<0>{}) && turn(Index<1>{}) && turn(Index<2>{}) && turn(Index<3>{})) {
+    }
+}
+
+// A barrier for LDS alone: reads under way stay under way.
+__device__ inline void lds_barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// What a block's products take of one token: its second operands.  Whole
+// groups of eight are read from the row's start where they lie past its end
+// (no branch about a read), and cleared before they are used.
+template <class W, bool VEC>
+__device__ inline void load_tokens(u32x4 (&b)[W::PRODUCTS], const uint16_t *row, uint32_t block, uint32_t g, uint32_t len)
 {
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const u32x4 a = w.operand(i);
+    for (uint32_t i = 0; i < W::PRODUCTS; i++) {
+        const uint32_t at = W::at(block, g, i);
+        b[i] = VEC ? *reinterpret_cast<const u32x4 *>(row + (at < len ? at : 0u)) : row8<false>(row, at, len);
+    }
+}
+template <class W, bool VEC>
+__device__ inline void clear_tokens(u32x4 (&b)[W::PRODUCTS], uint32_t block, uint32_t g, uint32_t len)
+{
+    if (!VEC || (block + 1) * W::VALUES <= len) return;
+#pragma unroll
+    for (uint32_t i = 0; i < W::PRODUCTS; i++)
+        if (W::at(block, g, i) >= len) b[i] = u32x4{0, 0, 0, 0};
+}
+
+template <class T, class C, uint32_t N>
+__device__ inline f32x4 up_products(const u32x4 (&p)[N], const u32x4 (&b)[N], f32x4 sum)
+{
+#pragma unroll
+    for (uint32_t i = 0; i < N; i++) {
+        if constexpr (__is_same(T, C)) {
+            sum = Frag<C>::mul(p[i], b[i], sum);
+        } else {   // f16 tokens against microscaled weights: two bf16 parts hold an f16 value exactly
+            uint16_t h[8], l[8];
+            _Float16 v[8];
+            __builtin_memcpy(v, &b[i], 16);
+#pragma unroll
+            for (int j = 0; j < 8; j++) split<C>((float)v[j], h[j], l[j]);
+            u32x4 bh, bl;
+            __builtin_memcpy(&bh, h, 16);
+            __builtin_memcpy(&bl, l, 16);
+            sum = Frag<C>::mul(p[i], bh, sum);
+            sum = Frag<C>::mul(p[i], bl, sum);
+        }
+    }
+    return sum;
+}
+
+// Gate and up rows: sub-tiles 2 i and 2 i + 1 of a wave's tile.
+template <class T, class W, bool VEC, int M, int NT, int DEPTH, bool SHARE>
+__global__ __launch_bounds__(64 * WAVES) void k_moe_up(MoeArgs a, MoeSpace m, uint32_t len, uint32_t slen)
+{
+    __shared__ __align__(16) uint8_t lds[WAVES][W::LDS];
+    __shared__ f32x4 sums[SHARE ? WAVES : 1][M][64];
+    __shared__ uint32_t who[MOE_MAX_TOKENS];   // the expert's tokens
+    typedef typename W::C C;
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), r = lane & 15u, g = lane >> 4;
+    constexpr uint32_t SPAN = M / 2 * 16;   // inner values of a tile
+    const Walk k = share_out<SHARE>(m, wave, (uint32_t)((m.inner + SPAN - 1) / SPAN), (a.hidden + W::VALUES - 1) / W::VALUES);
+    const uint32_t used = m.active[0], e = m.active[1 + blockIdx.y];
+    if (blockIdx.y >= used) return;
+    const uint64_t first = (uint64_t)e * 2u * a.inter;
+    const Rows up{static_cast<const char *>(a.up) + first * len, a.up_scales + first * slen, 2u * a.inter, len, slen};
+    W rows;
+    typename W::Block block[DEPTH];
+    u32x4 v[DEPTH][W::PRODUCTS];
+    for (uint32_t i = threadIdx.x; i < k.p1 - k.p0; i += 64 * WAVES) who[i] = m.slots[k.p0 + i];
+    __syncthreads();
+    // lanes without a token read the last one's values (their sums are not used)
+    auto token = [&](uint32_t place) {
+        return static_cast<const uint16_t *>(a.x) + (uint64_t)who[(place < k.p1 ? place : k.p1 - 1) - k.p0] * a.ld_x;
+    };
+    const uint16_t *x = token(k.p0 + r);
+    uint32_t held = k.p0, tile = NO_PLACE;   // whose rows x points to; the tile whose rows are read
+    auto read = [&](int d, const At &at, bool there) {
+        if (there && at.tile != tile) {
+            tile = at.tile;
+            uint32_t row[M];
+#pragma unroll
+            for (int i = 0; i < M; i++) {   // inner values past the last are padding: a row is read, zeros are stored
+                const uint32_t in = tile * SPAN + i / 2 * 16u;
+                row[i] = (in < a.inter ? in : 0u) + (i % 2 ? a.inter : 0u);
+            }
+            rows.begin(up, row);
+        }
+        if (at.p != held) {
+            held = at.p;
+            x = token(at.p + r);
+        }
+        rows.read(block[d], up, at.b, there);
+        load_tokens<W, VEC>(v[d], x, at.b, g, a.hidden);
+    };
+    f32x4 acc[M][NT] = {};
+    auto multiply = [&](int d, const At &at, uint32_t n) {
+        rows.turn(block[d], lds[wave], at.b);
+        clear_tokens<W, VEC>(v[d], at.b, g, a.hidden);
+        u32x4 p[M][W::PRODUCTS];
+#pragma unroll
+        for (int i = 0; i < M; i++) {
+            rows.operands(lds[wave], i, r, g, p[i]);
+            acc[i][0] = up_products<T, C>(p[i], v[d], acc[i][0]);
+        }
+#pragma unroll
+        for (int t = 1; t < NT; t++) {
+            if (t * 16u >= n) break;
+            u32x4 y[W::PRODUCTS];
+            load_tokens<W, VEC>(y, token(at.p + t * 16u + r), at.b, g, a.hidden);
+            clear_tokens<W, VEC>(y, at.b, g, a.hidden);
+#pragma unroll
+            for (int i = 0; i < M; i++) acc[i][t] = up_products<T, C>(p[i], y, acc[i][t]);
+        }
+    };
+    auto join = [&](const At &at, uint32_t n) {
 #pragma unroll
         for (int t = 0; t < NT; t++) {
-            const u32x4 b = row8<VEC>(x[t], W::at(step, g, i), end);
-            if constexpr (__is_same(T, typename W::C)) {
-                acc[t] = Frag<T>::mul(a, b, acc[t]);
-            } else {   // f16 tokens against microscaled weights: two bf16 parts hold an f16 value exactly
-                uint16_t h[8], l[8];
-                _Float16 v[8];
-                __builtin_memcpy(v, &b, 16);
+            if (t * 16u >= n) break;
+            f32x4 s[M];
 #pragma unroll
-                for (int q = 0; q < 8; q++) split<__bf16>((float)v[q], h[q], l[q]);
-                u32x4 bh, bl;
-                __builtin_memcpy(&bh, h, 16);
-                __builtin_memcpy(&bl, l, 16);
-                acc[t] = Frag<__bf16>::mul(a, bh, acc[t]);
-                acc[t] = Frag<__bf16>::mul(a, bl, acc[t]);
+            for (int i = 0; i < M; i++) {
+                s[i] = acc[i][t];
+                acc[i][t] = f32x4{0, 0, 0, 0};
+            }
+            if constexpr (SHARE) {
+                lds_barrier();   // the sums before have been read
+#pragma unroll
+                for (int i = 0; i < M; i++) sums[wave][i][lane] = s[i];
+                lds_barrier();
+                if (wave != 0) continue;
+#pragma unroll
+                for (int i = 0; i < M; i++)
+#pragma unroll
+                    for (int w = 1; w < WAVES; w++) s[i] += sums[w][i][lane];
+            }
+            if (t * 16u + r >= n) continue;
+#pragma unroll
+            for (int i = 0; i < M / 2; i++) {
+                const uint32_t i0 = at.tile * SPAN + i * 16u + g * 4u;
+                if (i0 >= m.inner) continue;
+                const f32x4 gate = s[2 * i], lift = s[2 * i + 1];
+                uint16_t hi[4], lo[4];
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const float h = i0 + q < a.inter ? gate[q] / (1.f + expf(-gate[q])) * lift[q] : 0.f;
+                    split<C>(h, hi[q], lo[q]);
+                }
+                uint32_t product, group;
+                W::place(i0, product, group);
+                const uint64_t to =
+                    (((uint64_t)(k.p0 / 16 + blockIdx.y + (at.p - k.p0) / 16 + t) * (m.inner / 32) + product) * 64u + group * 16u + r) * 8u + i0 % 8;
+                __builtin_memcpy(__builtin_assume_aligned(m.hi + to, 8), hi, 8);
+                __builtin_memcpy(__builtin_assume_aligned(m.lo + to, 8), lo, 8);
             }
         }
-    }
+    };
+    walk<NT, DEPTH>(k, read, multiply, join);
 }
 
-template <class T, class W, bool VEC, int NT>
-__device__ inline void up_tile(const MoeArgs &a, const MoeSpace &m, const uint16_t *gate, const uint16_t *lift, const uint8_t *gs,
-                               const uint8_t *ls, uint32_t p0, uint32_t n, uint32_t i0, f32x4 *sums)
+template <class W, int M, int NT, int DEPTH, bool SHARE>
+__global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, uint32_t len, uint32_t slen)
 {
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane & 15u, g = lane >> 4;
-    const uint16_t *x[NT];
+    __shared__ __align__(16) uint8_t lds[WAVES][W::LDS];
+    __shared__ f32x4 sums[SHARE ? WAVES : 1][M][64];
+    typedef typename W::C C;
+    constexpr uint32_t N = W::PRODUCTS, SPAN = M * 16;
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), r = lane & 15u, g = lane >> 4;
+    const Walk k = share_out<SHARE>(m, wave, (a.hidden + SPAN - 1) / SPAN, (uint32_t)(m.inner / W::VALUES));
+    const uint32_t used = m.active[0], e = m.active[1 + blockIdx.y];
+    if (blockIdx.y >= used) return;
+    const uint64_t first = (uint64_t)e * a.hidden;
+    const Rows down{static_cast<const char *>(a.down) + first * len, a.down_scales + first * slen, a.hidden, len, slen};
+    W rows;
+    typename W::Block block[DEPTH];
+    u32x4 hv[DEPTH][N], lv[DEPTH][N];
+    uint32_t tile = NO_PLACE;   // the tile whose rows are read
+    const uint32_t products = (uint32_t)(m.inner / 32);
+    // lanes without a token read the last one's values (their sums are not used)
+    auto inner = [&](u32x4 (&h)[N], u32x4 (&l)[N], const At &at, uint32_t t) {
+        const uint32_t n = k.p1 - at.p - t * 16u, who = r < n ? r : n - 1;
+        const uint64_t from = ((uint64_t)(k.p0 / 16 + blockIdx.y + (at.p - k.p0) / 16 + t) * products + at.b * N) * 64u + g * 16u + who;
 #pragma unroll
-    for (int t = 0; t < NT; t++) {
-        const uint32_t at = t * 16u + r < n ? t * 16u + r : n - 1;
-        x[t] = static_cast<const uint16_t *>(a.x) + (uint64_t)m.slots[p0 + at] * a.ld_x;
-    }
-    const uint32_t steps = (a.hidden + STEP - 1) / STEP;
-    const uint32_t per = (steps + WAVES - 1) / WAVES;
-    const uint32_t s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
-    f32x4 ga[NT] = {}, ua[NT] = {};
-    for (uint32_t s = s0; s < s1; s++) {
-        W gw, uw;
-        gw.load(gate, gs, s, g, a.hidden);
-        uw.load(lift, ls, s, g, a.hidden);
-        step_x<T, W, VEC, NT>(gw, x, s, g, a.hidden, ga);
-        step_x<T, W, VEC, NT>(uw, x, s, g, a.hidden, ua);
-    }
-    __syncthreads();   // the sums of the tokens before have been read
-#pragma unroll
-    for (int t = 0; t < NT; t++) {
-        sums[(wave * 2 * NT + t) * 64 + lane] = ga[t];
-        sums[(wave * 2 * NT + NT + t) * 64 + lane] = ua[t];
-    }
-    __syncthreads();
-    if (threadIdx.x < NT * 64) {
-        const uint32_t t = threadIdx.x >> 6;
-        f32x4 gv = {}, uv = {};
-#pragma unroll
-        for (int w = 0; w < WAVES; w++) {
-            gv += sums[(w * 2 * NT + t) * 64 + lane];
-            uv += sums[(w * 2 * NT + NT + t) * 64 + lane];
+        for (uint32_t i = 0; i < N; i++) {
+            h[i] = reinterpret_cast<const u32x4 *>(m.hi)[from + i * 64u];
+            l[i] = reinterpret_cast<const u32x4 *>(m.lo)[from + i * 64u];
         }
-        if (t * 16u + r < n) {
-            const uint64_t at = (uint64_t)(p0 + t * 16u + r) * m.inner + i0 + g * 4u;
-            uint16_t hi[4], lo[4];
+    };
+    auto read = [&](int d, const At &at, bool there) {
+        if (there && at.tile != tile) {
+            tile = at.tile;
+            uint32_t row[M];
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const float v = i0 + g * 4 + i < a.inter ? gv[i] / (1.f + expf(-gv[i])) * uv[i] : 0.f;
-                split<typename W::C>(v, hi[i], lo[i]);
-            }
-            __builtin_memcpy(__builtin_assume_aligned(m.hi + at, 8), hi, 8);
-            __builtin_memcpy(__builtin_assume_aligned(m.lo + at, 8), lo, 8);
+            for (int i = 0; i < M; i++) row[i] = tile * SPAN + i * 16u;
+            rows.begin(down, row);
         }
-    }
-}
-
-// A workgroup: 16 inner values of one expert in use, for all its tokens.
-template <class T, class W, bool VEC>
-__global__ __launch_bounds__(64 * WAVES) void k_moe_up(MoeArgs a, MoeSpace m)
-{
-    __shared__ f32x4 sums[WAVES * 2 * TILES * 64];
-    if (blockIdx.y >= m.active[0]) return;
-    const uint32_t e = m.active[1 + blockIdx.y], r = threadIdx.x & 15u;
-    const uint32_t p0 = m.first[blockIdx.y], p1 = m.first[blockIdx.y + 1];
-    const uint32_t i0 = blockIdx.x * 16u;   // inner values past the last are padding: rows clamped, zeros stored
-    const uint32_t row = i0 + r < a.inter ? i0 + r : a.inter - 1;
-    const uint64_t bytes = W::MX ? mx_code_bytes(a.hidden) : a.hidden * 2ull, sb = mx_scale_bytes(a.hidden);
-    const uint64_t gr = (uint64_t)e * 2u * a.inter + row, ur = gr + a.inter;
-    const uint16_t *gate = reinterpret_cast<const uint16_t *>(static_cast<const char *>(a.up) + gr * bytes);
-    const uint16_t *lift = reinterpret_cast<const uint16_t *>(static_cast<const char *>(a.up) + ur * bytes);
-    const uint8_t *gs = W::MX ? a.up_scales + gr * sb : nullptr, *ls = W::MX ? a.up_scales + ur * sb : nullptr;
-    for (uint32_t p = p0; p < p1; p += 16 * TILES) {
-        const uint32_t n = p1 - p < 16 * TILES ? p1 - p : 16 * TILES;
-        if (n <= 16) up_tile<T, W, VEC, 1>(a, m, gate, lift, gs, ls, p, n, i0, sums);
-        else if (n <= 32) up_tile<T, W, VEC, 2>(a, m, gate, lift, gs, ls, p, n, i0, sums);
-        else up_tile<T, W, VEC, 4>(a, m, gate, lift, gs, ls, p, n, i0, sums);
-    }
-}
-
-// ---- down ---------------------------------------------------------------------------
-
-template <class T, class W, int NT>
-__device__ inline void down_tile(const MoeArgs &a, const MoeSpace &m, const uint16_t *row, const uint8_t *sc, uint32_t p0, uint32_t n,
-                                 uint32_t h0, f32x4 *sums)
-{
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane & 15u, g = lane >> 4;
-    const uint16_t *hi[NT], *lo[NT];
+        rows.read(block[d], down, at.b, there);
+        inner(hv[d], lv[d], at, 0);
+    };
+    f32x4 acc[M][NT] = {}, rest[M][NT] = {};
+    auto multiply = [&](int d, const At &at, uint32_t n) {
+        rows.turn(block[d], lds[wave], at.b);
+        u32x4 p[M][N];
 #pragma unroll
-    for (int t = 0; t < NT; t++) {
-        const uint64_t at = (uint64_t)(p0 + (t * 16u + r < n ? t * 16u + r : n - 1)) * m.inner;
-        hi[t] = m.hi + at;
-        lo[t] = m.lo + at;
-    }
-    const uint32_t steps = (a.inter + STEP - 1) / STEP;
-    const uint32_t per = (steps + WAVES - 1) / WAVES;
-    const uint32_t s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
-    f32x4 acc[NT] = {}, rest[NT] = {};
-    for (uint32_t s = s0; s < s1; s++) {
-        W w;
-        w.load(row, sc, s, g, a.inter);
+        for (int i = 0; i < M; i++) {
+            rows.operands(lds[wave], i, r, g, p[i]);
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const u32x4 x = w.operand(i);
-            const uint32_t k = W::at(s, g, i);
-#pragma unroll
-            for (int t = 0; t < NT; t++) {
-                acc[t] = Frag<typename W::C>::mul(x, *reinterpret_cast<const u32x4 *>(hi[t] + k), acc[t]);
-                rest[t] = Frag<typename W::C>::mul(x, *reinterpret_cast<const u32x4 *>(lo[t] + k), rest[t]);
+            for (uint32_t j = 0; j < N; j++) {
+                acc[i][0] = Frag<C>::mul(p[i][j], hv[d][j], acc[i][0]);
+                rest[i][0] = Frag<C>::mul(p[i][j], lv[d][j], rest[i][0]);
             }
         }
-    }
-    __syncthreads();
 #pragma unroll
-    for (int t = 0; t < NT; t++) sums[(wave * NT + t) * 64 + lane] = acc[t] * Parts<typename W::C>::HI + rest[t] * Parts<typename W::C>::LO;
-    __syncthreads();
-    if (threadIdx.x < NT * 64) {
-        const uint32_t t = threadIdx.x >> 6;
-        f32x4 v = {};
+        for (int t = 1; t < NT; t++) {
+            if (t * 16u >= n) break;
+            u32x4 h[N], l[N];
+            inner(h, l, at, t);
 #pragma unroll
-        for (int w = 0; w < WAVES; w++) v += sums[(w * NT + t) * 64 + lane];
-        if (t * 16u + r < n) {
-            float *out = m.outs + (uint64_t)(p0 + t * 16u + r) * a.hidden + h0 + g * 4u;
+            for (int i = 0; i < M; i++)
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-                if (h0 + g * 4 + i < a.hidden) out[i] = v[i];
+                for (uint32_t j = 0; j < N; j++) {
+                    acc[i][t] = Frag<C>::mul(p[i][j], h[j], acc[i][t]);
+                    rest[i][t] = Frag<C>::mul(p[i][j], l[j], rest[i][t]);
+                }
         }
-    }
+    };
+    auto join = [&](const At &at, uint32_t n) {
+#pragma unroll
+        for (int t = 0; t < NT; t++) {
+            if (t * 16u >= n) break;
+            f32x4 s[M];
+#pragma unroll
+            for (int i = 0; i < M; i++) {
+                s[i] = acc[i][t] * Parts<C>::HI + rest[i][t] * Parts<C>::LO;
+                acc[i][t] = rest[i][t] = f32x4{0, 0, 0, 0};
+            }
+            if constexpr (SHARE) {
+                lds_barrier();   // the sums before have been read
+#pragma unroll
+                for (int i = 0; i < M; i++) sums[wave][i][lane] = s[i];
+                lds_barrier();
+                if (wave != 0) continue;
+#pragma unroll
+                for (int i = 0; i < M; i++)
+#pragma unroll
+                    for (int q = 1; q < WAVES; q++) s[i] += sums[q][i][lane];
+            }
+            if (t * 16u + r >= n) continue;
+            const uint32_t place = at.p + t * 16u + r;
+            const float share = m.shares[place];
+#pragma unroll
+            for (int i = 0; i < M; i++) {
+                const uint32_t h = at.tile * SPAN + i * 16u + g * 4u;
+                float *to = m.outs + (uint64_t)place * a.hidden + h;
+                const f32x4 o = s[i] * share;
+                if (a.hidden % 4 == 0) {
+                    if (h < a.hidden) *reinterpret_cast<f32x4 *>(to) = o;
+                    continue;
+                }
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                    if (h + q < a.hidden) to[q] = o[q];
+            }
+        }
+    };
+    walk<NT, DEPTH>(k, read, multiply, join);
 }
 
-// A workgroup: 16 outputs of one expert in use, for all its tokens.
-template <class T, class W>
-__global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m)
-{
-    __shared__ f32x4 sums[WAVES * TILES * 64];
-    if (blockIdx.y >= m.active[0]) return;
-    const uint32_t e = m.active[1 + blockIdx.y], r = threadIdx.x & 15u;
-    const uint32_t p0 = m.first[blockIdx.y], p1 = m.first[blockIdx.y + 1];
-    const uint32_t h0 = blockIdx.x * 16u;
-    const uint64_t bytes = W::MX ? mx_code_bytes(a.inter) : a.inter * 2ull;
-    const uint64_t row = (uint64_t)e * a.hidden + (h0 + r < a.hidden ? h0 + r : a.hidden - 1);
-    const uint16_t *w = reinterpret_cast<const uint16_t *>(static_cast<const char *>(a.down) + row * bytes);
-    const uint8_t *sc = W::MX ? a.down_scales + row * mx_scale_bytes(a.inter) : nullptr;
-    for (uint32_t p = p0; p < p1; p += 16 * TILES) {
-        const uint32_t n = p1 - p < 16 * TILES ? p1 - p : 16 * TILES;
-        if (n <= 16) down_tile<T, W, 1>(a, m, w, sc, p, n, h0, sums);
-        else if (n <= 32) down_tile<T, W, 2>(a, m, w, sc, p, n, h0, sums);
-        else down_tile<T, W, 4>(a, m, w, sc, p, n, h0, sums);
-    }
-}
-
-// Each token's weighted sum over its picks, in their order; zeros without any.
+// Each token's sum over its picks, in their order; zeros without any.
 template <class T>
-__global__ __launch_bounds__(256) void k_moe_join(MoeArgs a, MoeSpace m)
+__global__ __launch_bounds__(256) void k_moe_sum(MoeArgs a, MoeSpace m)
 {
     const uint32_t t = blockIdx.y, h = blockIdx.x * 256u + threadIdx.x;
     if (h >= a.hidden) return;
     float v = 0.f;
+#pragma unroll 4
     for (uint32_t j = 0; j < a.topk; j++) {
-        const int32_t p = m.place[t * a.topk + j];
-        if (p >= 0) v += m.weights[t * a.topk + j] * m.outs[(uint64_t)p * a.hidden + h];
+        const uint32_t p = m.place[t * a.topk + j];
+        if (p != NO_PLACE) v += m.outs[(uint64_t)p * a.hidden + h];
     }
     static_cast<T *>(a.y)[(uint64_t)t * a.ld_y + h] = Elem<T>::put(v);
 }
 
-template <class T, class WU, class WD, bool VEC>
+// Tiles of all experts that may be in use from which on a wave has tiles of
+// its own: enough of them to keep every compute unit's waves busy.
+constexpr uint32_t OWN_TILES = 1u << 30;
+
+template <class T, class WU, class WD, bool VEC, int MU, int MD, int DU, int DD, int NT>
 hipError_t experts_as(const MoeArgs &a, const MoeSpace &m, hipStream_t s)
 {
     const uint64_t places = (uint64_t)a.tokens * a.topk;
     const uint32_t most = places < a.experts ? (uint32_t)places : a.experts;
-    k_moe_up<T, WU, VEC><<<dim3((uint32_t)(m.inner / 16), most), 64 * WAVES, 0, s>>>(a, m);
-    k_moe_down<T, WD><<<dim3((a.hidden + 15) / 16, most), 64 * WAVES, 0, s>>>(a, m);
-    k_moe_join<T><<<dim3((a.hidden + 255) / 256, a.tokens), 256, 0, s>>>(a, m);
+    const bool mx = a.up_scales != nullptr;
+    const uint32_t ul = mx ? (uint32_t)mx_code_bytes(a.hidden) : a.hidden * 2u, us = mx ? (uint32_t)mx_scale_bytes(a.hidden) : 0u;
+    const uint32_t dl = mx ? (uint32_t)mx_code_bytes(a.inter) : a.inter * 2u, ds = mx ? (uint32_t)mx_scale_bytes(a.inter) : 0u;
+    const uint32_t up = (uint32_t)((m.inner + MU * 8 - 1) / (MU * 8)), down = (a.hidden + MD * 16 - 1) / (MD * 16);
+    if ((uint64_t)up * most < OWN_TILES) k_moe_up<T, WU, VEC, MU, NT, DU, true><<<dim3(up, most), 64 * WAVES, 0, s>>>(a, m, ul, us);
+    else k_moe_up<T, WU, VEC, MU, NT, DU, false><<<dim3((up + WAVES - 1) / WAVES, most), 64 * WAVES, 0, s>>>(a, m, ul, us);
+    if ((uint64_t)down * most < OWN_TILES) k_moe_down<WD, MD, NT, DD, true><<<dim3(down, most), 64 * WAVES, 0, s>>>(a, m, dl, ds);
+    else k_moe_down<WD, MD, NT, DD, false><<<dim3((down + WAVES - 1) / WAVES, most), 64 * WAVES, 0, s>>>(a, m, dl, ds);
+    k_moe_sum<T><<<dim3((a.hidden + 255) / 256, a.tokens), 256, 0, s>>>(a, m);
     return hipGetLastError();
+}
+
+// Tiles of 16 tokens that share one reading of the weights: one where experts
+// have eight tokens on average at most (few have more than 16, and theirs are
+// read again), four otherwise, at the price of registers for reads ahead.
+template <class T, class WU, class WD, bool VEC, int MU, int MD, int DU, int DD>
+hipError_t experts_of(const MoeArgs &a, const MoeSpace &m, hipStream_t s)
+{
+    if (a.tokens <= 16 || (uint64_t)a.tokens * a.topk <= 8ull * a.experts) return experts_as<T, WU, WD, VEC, MU, MD, DU, DD, 1>(a, m, s);
+    return experts_as<T, WU, WD, VEC, MU, MD, 2, 2, 4>(a, m, s);
+}
+
+template <int LANES, int V>
+hipError_t pick_as(const MoeArgs &a, const MoeSpace &m, hipStream_t s)
+{
+    auto room = [](uint32_t tokens, uint32_t experts, uint32_t topk) { return (tokens + 63) / 64 * experts * 8u + experts * 4u + tokens * topk * 8u; };
+    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_moe_pick<LANES, V>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                       room(MOE_MAX_TOKENS, ROUTE_MAX_EXPERTS, ROUTE_MAX_TOPK));
+    if (once != hipSuccess) return once;
+    k_moe_pick<LANES, V><<<1, 64 * PICK_WAVES, room(a.tokens, a.experts, a.topk), s>>>(a, m);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t picks(const MoeArgs &a, const MoeSpace &m, bool vec, hipStream_t s)
+{
+    const dim3 grid((a.experts + 15) / 16, m.splits, (a.tokens + 15) / 16);
+    if (vec) k_moe_logits<T, true><<<grid, 64 * WAVES, 0, s>>>(a, m);
+    else k_moe_logits<T, false><<<grid, 64 * WAVES, 0, s>>>(a, m);
+    if (a.experts <= 64) return pick_as<16, 4>(a, m, s);
+    if (a.experts <= 128) return pick_as<16, 8>(a, m, s);
+    if (a.experts <= NARROW_EXPERTS) return pick_as<16, 16>(a, m, s);
+    if (a.experts <= 512) return pick_as<64, 8>(a, m, s);
+    return pick_as<64, 16>(a, m, s);
 }
 
 template <class T>
@@ -479,21 +874,16 @@ hipError_t moe_as(const MoeArgs &a, hipStream_t s)
     MoeSpace m;
     carve(m, a.ws, a.tokens, a.experts, a.topk, a.hidden, a.inter);
     auto aligned = [](const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
-    // whole groups of eight values: the router's and the tokens' rows are read 16 bytes at a time
+    // whole groups of eight values: rows are read 16 bytes at a time
     const bool vx = aligned(a.x) && a.ld_x % 8 == 0 && a.hidden % 8 == 0;
-    const bool vr = vx && aligned(a.router);
-    const dim3 grid((a.experts + 15) / 16, m.splits, (a.tokens + 15) / 16);
-    if (vr) k_moe_logits<T, true><<<grid, 64 * WAVES, 0, s>>>(a, m);
-    else k_moe_logits<T, false><<<grid, 64 * WAVES, 0, s>>>(a, m);
-    if (a.experts <= 64) k_moe_pick<1><<<1, 64 * PICK_WAVES, 0, s>>>(a, m);
-    else if (a.experts <= 128) k_moe_pick<2><<<1, 64 * PICK_WAVES, 0, s>>>(a, m);
-    else if (a.experts <= 256) k_moe_pick<4><<<1, 64 * PICK_WAVES, 0, s>>>(a, m);
-    else if (a.experts <= 512) k_moe_pick<8><<<1, 64 * PICK_WAVES, 0, s>>>(a, m);
-    else k_moe_pick<16><<<1, 64 * PICK_WAVES, 0, s>>>(a, m);
-    if (a.up_scales) return vx ? experts_as<T, Micro, Micro, true>(a, m, s) : experts_as<T, Micro, Micro, false>(a, m, s);
-    const bool vu = vx && aligned(a.up), vd = aligned(a.down) && a.inter % 8 == 0;
-    if (vu && vd) return experts_as<T, Plain<T, true>, Plain<T, true>, true>(a, m, s);
-    return experts_as<T, Plain<T, false>, Plain<T, false>, false>(a, m, s);
+    const hipError_t e = picks<T>(a, m, vx && aligned(a.router), s);
+    if (e != hipSuccess) return e;
+    if (a.up_scales) {
+        if (vx) return experts_of<T, Micro<4>, Micro<4>, true, 4, 4, 3, 2>(a, m, s);
+        return experts_of<T, Micro<4>, Micro<4>, false, 4, 4, 2, 2>(a, m, s);
+    }
+    if (vx && aligned(a.up) && aligned(a.down) && a.inter % 8 == 0) return experts_of<T, Plain<T, 2>, Plain<T, 2>, true, 2, 2, 3, 3>(a, m, s);
+    return experts_of<T, Loose<T, 2>, Loose<T, 2>, false, 2, 2, 2, 2>(a, m, s);
 }
 
 }  // namespace

@@ -43,6 +43,7 @@ constexpr uint32_t ROUTE_ROWS = 64;   // rows of one workgroup: one bit each in 
 // The layer's envelope: "a few tokens".
 constexpr uint32_t MOE_MAX_TOKENS = 256;
 constexpr uint32_t MOE_MAX_DIM = 1u << 20;   // hidden and inner size
+constexpr uint64_t MOE_MAX_MATRIX = 1ull << 29;   // their product: an expert's rows stay within 32-bit offsets
 
 struct MxQuantizeArgs {
     const void *x;

@@ -133,6 +133,7 @@ pccl_status check_layer(pccl_ctx *c, uint32_t tokens, uint32_t experts, uint32_t
     LIMIT(tokens <= MOE_MAX_TOKENS, "%u tokens (limit %u)", tokens, MOE_MAX_TOKENS);
     NEED(hidden > 0 && inter > 0, "hidden %u, inter %u", hidden, inter);
     LIMIT(hidden <= MOE_MAX_DIM && inter <= MOE_MAX_DIM, "hidden %u, inter %u (limit %u)", hidden, inter, MOE_MAX_DIM);
+    LIMIT((uint64_t)hidden * inter <= MOE_MAX_MATRIX, "hidden %u x inter %u (limit 2^29 values)", hidden, inter);
     return PCCL_OK;
 }
 
@@ -229,7 +230,7 @@ pccl_status pccl_moe_route(pccl_ctx *c, const void *logits, pccl_dtype dtype, ui
             NEED(ids && aligned(ids, 4), "ids are null or misaligned");
             NEED(order && aligned(order, 4), "order is null or misaligned");
         }
-        TRY(check_grid(c, (tokens + ROUTE_ROWS - 1) / ROUTE_ROWS, 256));
+        TRY(check_grid(c, (tokens + ROUTE_ROWS - 1) / ROUTE_ROWS, 1024));
         TRY(check_space(c, workspace, workspace_bytes, route_workspace(tokens, experts)));
         TRY(on_device(c));
         const RouteArgs a{logits, tokens, ld, experts, topk, normalize ? 1u : 0u, token_mask, weights, ids, counts, order, (uint32_t *)workspace};

@@ -1,102 +1,167 @@
 // The router's row step, shared by the router and the mixture-of-experts
-// layer: a wave holds a row of logits, VPL neighbouring ones a lane, as
-// 32-bit keys that order like the logits, and draws the largest k.
+// layer: the lanes of a row of logits (16 up to 256 experts, four rows a wave;
+// a whole wave beyond) hold V neighbouring ones each as whole numbers that
+// order like them, and draw the largest k.
 #pragma once
 
 #include "pccl_ops.h"
 
 namespace pccl {
 
-constexpr uint32_t KEY_EMPTY = 0x007FFFFFu;   // minus infinity; nothing at or below it is drawn
+// Logits as keys that order like them, a NaN above everything, both zeros
+// alike; nothing at or below EMPTY (minus infinity) is drawn.  A 16-bit logit
+// leaves room for its index, lowest first: such keys differ, so the largest
+// one says where it stands.
+template <class T>
+struct Key;
+template <>
+struct Key<float> {
+    static constexpr uint32_t EMPTY = 0x007FFFFFu;
+    static constexpr bool INDEXED = false;
+    static __device__ uint32_t of(float v, uint32_t)
+    {
+        if (v != v) return 0xFFFFFFFFu;
+        const uint32_t b = __float_as_uint(v + 0.f);
+        return b & 0x80000000u ? ~b : b | 0x80000000u;
+    }
+    static __device__ float value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+    static __device__ uint32_t index(uint32_t) { return 0; }
+};
+template <class T>
+struct Key16 {
+    static constexpr bool INDEXED = true;
+    static __device__ uint32_t of(T v, uint32_t e)
+    {
+        uint32_t b = __builtin_bit_cast(uint16_t, v);
+        b = b & 0x8000u ? 0x10000u - b : b + 0x8000u;   // minus zero lands on plus zero
+        if (v != v) b = 0xFFFFu;
+        return b << 16 | (0xFFFFu - e);
+    }
+    static __device__ float value(uint32_t k)
+    {
+        k >>= 16;
+        const uint16_t b = (uint16_t)(k & 0x8000u ? k - 0x8000u : 0x10000u - k);
+        return (float)__builtin_bit_cast(T, b);
+    }
+    static __device__ uint32_t index(uint32_t k) { return 0xFFFFu - (k & 0xFFFFu); }
+};
+template <>
+struct Key<__bf16> : Key16<__bf16> {
+    static constexpr uint32_t EMPTY = 0x0080FFFFu;   // minus infinity, any index
+};
+template <>
+struct Key<_Float16> : Key16<_Float16> {
+    static constexpr uint32_t EMPTY = 0x0400FFFFu;
+};
 
-// A float as a whole number that orders like it: a NaN above everything,
-// both zeros alike.
-__device__ inline uint32_t key_of(float v)
-{
-    if (v != v) return 0xFFFFFFFFu;
-    const uint32_t b = __float_as_uint(v + 0.f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ inline float of_key(uint32_t k)
-{
-    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
-}
-
-// Reductions over a wave on the lanes' own paths (rows of 16, then across);
-// the result is uniform.
 template <int CTRL, int ROWS>
 __device__ inline uint32_t dpp(uint32_t v)
 {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
 }
-__device__ inline uint32_t dpp_max(uint32_t v)
+
+// Reductions over the LANES lanes of a row, on the lanes' own paths; every
+// lane of the row gets the result.
+template <int LANES, class Op>
+__device__ inline uint32_t reduce(uint32_t v, Op op)
 {
-    auto up = [&](uint32_t w) { v = w > v ? w : v; };
-    up(dpp<0x111, 0xF>(v));   // one, two, four and eight lanes along a row of 16
-    up(dpp<0x112, 0xF>(v));
-    up(dpp<0x114, 0xF>(v));
-    up(dpp<0x118, 0xF>(v));
-    up(dpp<0x142, 0xA>(v));   // a row's last lane into the next row
-    up(dpp<0x143, 0xC>(v));   // the lower half's last lane into the upper half
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+    if constexpr (LANES == 16) {   // rotations within 16 lanes
+        v = op(v, dpp<0x128, 0xF>(v));
+        v = op(v, dpp<0x124, 0xF>(v));
+        v = op(v, dpp<0x122, 0xF>(v));
+        return op(v, dpp<0x121, 0xF>(v));
+    } else {                       // shifts (zeros come in), a row's last lane into the next, the lower half's into the upper
+        v = op(v, dpp<0x111, 0xF>(v));
+        v = op(v, dpp<0x112, 0xF>(v));
+        v = op(v, dpp<0x114, 0xF>(v));
+        v = op(v, dpp<0x118, 0xF>(v));
+        v = op(v, dpp<0x142, 0xA>(v));
+        v = op(v, dpp<0x143, 0xC>(v));
+        return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+    }
 }
-__device__ inline float dpp_sum(float v)
+template <int LANES>
+__device__ inline uint32_t row_max(uint32_t v)
 {
-    auto up = [&](uint32_t w) { v += __uint_as_float(w); };
-    up(dpp<0x111, 0xF>(__float_as_uint(v)));
-    up(dpp<0x112, 0xF>(__float_as_uint(v)));
-    up(dpp<0x114, 0xF>(__float_as_uint(v)));
-    up(dpp<0x118, 0xF>(__float_as_uint(v)));
-    up(dpp<0x142, 0xA>(__float_as_uint(v)));
-    up(dpp<0x143, 0xC>(__float_as_uint(v)));
-    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
+    return reduce<LANES>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+template <int LANES>
+__device__ inline float row_sum(float v)
+{
+    return __uint_as_float(reduce<LANES>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
 }
 
-// Draws the k largest of the row's keys, ties to the lowest index, and gives
-// lane j the j-th pick's index (-1: none left) and weight: the softmax over
-// the whole row or, normalised, over the picks.  One pass of the statistics in
-// 32 bits; a row with nothing above minus infinity has no picks.
-template <int VPL>
-__device__ inline void topk_row(uint32_t (&key)[VPL], uint32_t k, bool normalize, uint32_t lane, int32_t &id, float &weight)
+// Lanes of a row for so many experts, and the picks a lane may have to hold.
+constexpr uint32_t NARROW_EXPERTS = 256;
+template <int LANES>
+constexpr int picks_held() { return LANES == 16 ? (int)ROUTE_MAX_TOPK / 16 : 1; }
+
+// Draws the k largest of the row's keys, ties to the lowest index; lane `sub`
+// of the row gets pick sub (and 16 + sub where a row has 16 lanes): its index
+// (-1: none left) and weight, the softmax over the whole row or, normalised,
+// over the picks, with its statistics in 32 bits.  A row with nothing above
+// minus infinity has no picks.
+template <class T, int LANES, int V>
+__device__ inline void topk_row(uint32_t (&key)[V], uint32_t k, bool normalize, uint32_t sub, int32_t (&id)[picks_held<LANES>()],
+                                float (&weight)[picks_held<LANES>()])
 {
-    uint32_t local = 0;
+    typedef Key<T> K;
+    constexpr int HELD = picks_held<LANES>();
+    auto local_max = [&]() {
+        uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < VPL; i++) local = key[i] > local ? key[i] : local;
-    uint32_t best = dpp_max(local);
-    const float top = of_key(best);
+        for (int i = 0; i < V; i++) m = key[i] > m ? key[i] : m;
+        return m;
+    };
+    uint32_t best = row_max<LANES>(local_max());
+    const float top = K::value(best);
     float total = 0.f;
-    if (!normalize && best > KEY_EMPTY) {
+    if (!normalize) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < VPL; i++)
-            if (key[i] > KEY_EMPTY) sum += expf(of_key(key[i]) - top);
-        total = dpp_sum(sum);
+        for (int i = 0; i < V; i++) sum += key[i] > K::EMPTY ? expf(K::value(key[i]) - top) : 0.f;
+        total = row_sum<LANES>(sum);
     }
-    id = -1;
-    uint32_t got = KEY_EMPTY;
-    for (uint32_t j = 0; j < k && best > KEY_EMPTY; j++) {
-        int at = VPL;
+    uint32_t got[HELD];
 #pragma unroll
-        for (int i = VPL - 1; i >= 0; i--)
-            if (key[i] == best) at = i;
-        const uint64_t have = __ballot(at < VPL);
-        const int first = __ffsll((unsigned long long)have) - 1;
-        const int pick = __builtin_amdgcn_readlane(at, first);
-        if (lane == j) {
-            id = first * VPL + pick;
-            got = best;
-        }
-        local = 0;
-#pragma unroll
-        for (int i = 0; i < VPL; i++) {
-            if ((int)lane == first && i == pick) key[i] = 0;
-            local = key[i] > local ? key[i] : local;
-        }
-        best = dpp_max(local);
+    for (int h = 0; h < HELD; h++) {
+        id[h] = -1;
+        got[h] = 0;
     }
-    float e = got > KEY_EMPTY ? expf(of_key(got) - top) : 0.f;
-    if (normalize) total = dpp_sum(e);
-    weight = id >= 0 ? e / total : 0.f;
+    for (uint32_t j = 0; j < k; j++) {
+        if (LANES == 64 && best <= K::EMPTY) break;
+        uint32_t at;
+        if constexpr (K::INDEXED) {
+            at = K::index(best);
+#pragma unroll
+            for (int i = 0; i < V; i++) key[i] = key[i] == best ? 0u : key[i];
+        } else {
+            uint32_t mine = 0;   // the lowest index is the largest of the negated ones
+#pragma unroll
+            for (int i = V - 1; i >= 0; i--) mine = key[i] == best ? ~(sub * V + i) : mine;
+            at = ~row_max<LANES>(mine);
+#pragma unroll
+            for (int i = 0; i < V; i++) key[i] = at == sub * V + i ? 0u : key[i];
+        }
+#pragma unroll
+        for (int h = 0; h < HELD; h++)
+            if (sub + 16u * h == j) {
+                got[h] = best;
+                id[h] = best > K::EMPTY ? (int32_t)at : -1;
+            }
+        best = row_max<LANES>(local_max());
+    }
+    float e[HELD], sum = 0.f;
+#pragma unroll
+    for (int h = 0; h < HELD; h++) {
+        e[h] = id[h] >= 0 ? expf(K::value(got[h]) - top) : 0.f;
+        sum += e[h];
+    }
+    if (normalize) total = row_sum<LANES>(sum);
+#pragma unroll
+    for (int h = 0; h < HELD; h++) weight[h] = id[h] >= 0 ? e[h] / total : 0.f;
 }
 
 // Exclusive scan over the threads of a workgroup of WAVES waves; `sums` is

@@ -79,7 +79,8 @@ class Operators:
         return self._same("mask", mask, (tokens,), torch.uint8)
 
     def _stream(self):
-        return torch.cuda.current_stream(self.device).cuda_stream
+        # the address alone: building a torch.cuda.Stream takes longer than the smallest kernels
+        return torch._C._cuda_getCurrentRawStream(self._index)
 
     def _empty(self, shape, dtype):
         return torch.empty(shape, dtype=dtype, device=self.device)
