@@ -452,7 +452,7 @@ pccl_status pccl_mx_matmul_workspace(pccl_ctx *ctx, uint64_t m, uint64_t n, uint
 /*
  * out (m x n of `dtype`, row stride ld) = A B^T for packed A (m rows of k
  * values) and B (n rows of k values), summed in 32 bits and rounded once.  k =
- * 0 gives zeros.  A layer's forward product takes the packed rows of x and W,
+ * 0 gives zeros; k is at most 2^24.  A layer's forward product takes the packed rows of x and W,
  * its input gradient those of dy and of W's columns, its weight gradient those
  * of dy's and x's columns.
  */

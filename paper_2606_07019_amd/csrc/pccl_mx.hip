@@ -134,11 +134,11 @@ constexpr uint32_t TILE = 128;   // rows and columns of a workgroup's tile: one 
 // row; four lanes share a block of the rows' packing.  For the columns the
 // wave's part goes through LDS, where a lane then reads two columns of 32
 // rows.  Memory-bound: every value is read once for both directions.
-template <class T, bool VEC, bool ROWS, bool COLS>
+template <class T, bool VEC, bool ROWS>
 __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantizeArgs a, uint32_t col_tiles)
 {
-    __shared__ uint32_t part[COLS ? 4 : 1][COLS ? 32 * TILE * sizeof(T) / 4 : 1];
-    __shared__ uint8_t tsc[COLS ? TILE : 1][4];
+    __shared__ __align__(16) uint32_t part[4][32 * TILE * sizeof(T) / 4];
+    __shared__ __align__(16) uint8_t tsc[TILE][4];
     const T *x = static_cast<const T *>(a.x);
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const uint32_t tr = blockIdx.x / col_tiles, tc = blockIdx.x % col_tiles;
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantizeArgs a, uint32_t 
             for (int i = 0; i < Oct<T>::W; i++) o[p].w[i] = 0;
         }
     }
-    if (COLS) {
+    {
 #pragma unroll
         for (int p = 0; p < 8; p++) {
             u32x4 *q = reinterpret_cast<u32x4 *>(&part[wave][((p * 4 + (lane >> 4)) * TILE + c0) * sizeof(T) / 4]);
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantizeArgs a, uint32_t 
             }
         }
     }
-    if (COLS) {
+    {
         __syncthreads();
         const uint64_t cbt = mx_code_bytes(a.rows), sbt = mx_scale_bytes(a.rows);
         const uint32_t c = lane * 2;
@@ -239,17 +239,71 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantizeArgs a, uint32_t 
                 }
             }
         }
+        // the columns' codes go out by way of LDS, 64 bytes of a column at a
+        // time; piece w of column c stands at (w + c / 2) % 4 of the column
+        __syncthreads();
+        u32x4 *out_lds = reinterpret_cast<u32x4 *>(part);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const uint64_t cc = (uint64_t)tc * TILE + c + h;
             tsc[c + h][wave] = (uint8_t)byte[h];
-            if (cc < a.cols) *reinterpret_cast<u32x4 *>(a.codes_t + cc * cbt + (uint64_t)tr * (TILE / 2) + wave * 16u) = out[h];
+            out_lds[(c + h) * 4u + ((wave + lane) & 3u)] = out[h];
         }
         __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < 2; i++) {
+            const uint32_t at = i * 64u + threadIdx.x / 4, w = threadIdx.x % 4;
+            const uint64_t cc = (uint64_t)tc * TILE + at;
+            if (cc < a.cols)
+                *reinterpret_cast<u32x4 *>(a.codes_t + cc * cbt + (uint64_t)tr * (TILE / 2) + w * 16u) = out_lds[at * 4u + ((w + at / 2) & 3u)];
+        }
         const uint64_t cc = (uint64_t)tc * TILE + threadIdx.x;
         if (threadIdx.x < TILE && cc < a.cols)
             *reinterpret_cast<uint32_t *>(a.scales_t + cc * sbt + (uint64_t)tr * 4u) =
                 *reinterpret_cast<const uint32_t *>(tsc[threadIdx.x]);
+    }
+}
+
+// The rows alone: a wave packs 512 values of eight rows at a time, so that what
+// it reads, its codes and its scales are contiguous (1 KiB, 256 and 16 bytes).
+template <class T, bool VEC>
+__global__ __launch_bounds__(256) void k_mx_rows(MxQuantizeArgs a, uint32_t chunks)
+{
+    const T *x = static_cast<const T *>(a.x);
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint64_t item = (uint64_t)blockIdx.x * 4u + (threadIdx.x >> 6);
+    const uint64_t row0 = item / chunks * 8u, col = item % chunks * 512u + lane * 8u;
+    const uint64_t cb = mx_code_bytes(a.cols), sb = mx_scale_bytes(a.cols);
+    if (row0 >= a.rows) return;
+    Oct<T> o[8];
+#pragma unroll
+    for (int p = 0; p < 8; p++) {
+        const uint64_t r = row0 + p;
+        if (r < a.rows && col < a.cols) {
+            o[p] = load8<T, VEC>(x + r * a.ld + col, a.cols - col);
+        } else {
+#pragma unroll
+            for (int i = 0; i < Oct<T>::W; i++) o[p].w[i] = 0;
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < 8; p++) {
+        const uint64_t r = row0 + p;
+        uint32_t t = top_of(o[p]);
+        uint32_t u = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0xB1, 0xF, 0xF, false);   // lanes 1 0 3 2 of four
+        t = u > t ? u : t;
+        u = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0x4E, 0xF, 0xF, false);            // lanes 2 3 0 1
+        t = u > t ? u : t;
+        const uint32_t byte = MxIn<T>::byte(t);
+        const uint32_t code = codes8(o[p], byte);
+        // four blocks' scales to a word, at the first of their sixteen lanes
+        uint32_t word = byte;
+        word |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)byte, 0x104, 0xF, 0xF, false) << 8;
+        word |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)byte, 0x108, 0xF, 0xF, false) << 16;
+        word |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)byte, 0x10C, 0xF, 0xF, false) << 24;
+        if (r < a.rows && col / 2 < cb) {
+            *reinterpret_cast<uint32_t *>(a.codes + r * cb + col / 2) = code;
+            if (lane % 16 == 0) *reinterpret_cast<uint32_t *>(a.scales + r * sb + col / MX_BLOCK) = word;
+        }
     }
 }
 
@@ -258,9 +312,15 @@ hipError_t quantize_as(const MxQuantizeArgs &a, hipStream_t s)
 {
     const uint32_t ct = (uint32_t)((a.cols + TILE - 1) / TILE), rt = (uint32_t)((a.rows + TILE - 1) / TILE);
     const dim3 grid(ct * rt);
-    if (a.codes && a.codes_t) k_mx_quantize<T, VEC, true, true><<<grid, 256, 0, s>>>(a, ct);
-    else if (a.codes) k_mx_quantize<T, VEC, true, false><<<grid, 256, 0, s>>>(a, ct);
-    else k_mx_quantize<T, VEC, false, true><<<grid, 256, 0, s>>>(a, ct);
+    if (!a.codes_t) {
+        const uint32_t chunks = (uint32_t)((a.cols + 511) / 512);
+        const uint64_t items = (a.rows + 7) / 8 * chunks;
+        k_mx_rows<T, VEC><<<dim3((uint32_t)((items + 3) / 4)), 256, 0, s>>>(a, chunks);
+    } else if (a.codes) {
+        k_mx_quantize<T, VEC, true><<<grid, 256, 0, s>>>(a, ct);
+    } else {
+        k_mx_quantize<T, VEC, false><<<grid, 256, 0, s>>>(a, ct);
+    }
     return hipGetLastError();
 }
 

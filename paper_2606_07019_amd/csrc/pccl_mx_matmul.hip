@@ -5,6 +5,11 @@
 // l % 16 of an operand, block l / 16 of the step (16 bytes of codes), and gets
 // four sums: rows 4 (l / 16) ... + 3 of the first operand, row l % 16 of the
 // second.  B goes first, so a lane's sums are neighbours in out.
+//
+// The form with 32 rows of each operand over 64 values of k is the faster one
+// (6.8 PFLOP/s from registers with random values, 4.3 for 16 rows) and serves
+// many rows: lane l gives row l % 32, one block, and gets sixteen sums, four
+// neighbours in rows 8 q + 4 (l / 32) of the first operand.
 #include "pccl_ops.h"
 
 namespace pccl {
@@ -15,6 +20,17 @@ __device__ inline f32x4 mfma_mx(u32x4 a, uint32_t as, u32x4 b, uint32_t bs, f32x
     const i32x8 x = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
     const i32x8 y = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, (int)as, 0, (int)bs);
+}
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// SEL: which byte of the words holds the scale.
+template <int SEL>
+__device__ inline f32x16 mfma_mx32(u32x4 a, uint32_t as, u32x4 b, uint32_t bs, f32x16 c)
+{
+    const i32x8 x = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
+    const i32x8 y = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, SEL, (int)as, SEL, (int)bs);
 }
 
 // Four neighbouring sums of row `row`, from column `col` on.
@@ -44,54 +60,107 @@ __device__ inline void store4(T *out, uint64_t ld, uint64_t row, uint64_t col, u
 
 // ---- few rows ----------------------------------------------------------------
 
-constexpr int SKINNY_WAVES = 8;
-
-// Up to 16 MT rows of A: bound by reading B once.  A workgroup has 16 rows of
-// B; its waves share out k, read both operands straight into registers (no
-// row of B is used twice, A's come from L2) and join their sums in LDS, in the
-// waves' order.
-template <class T, int MT>
-__global__ __launch_bounds__(64 * SKINNY_WAVES) void k_mx_skinny(MxMatmulArgs a, bool vec)
+// Four neighbouring sums of row `row`, in the output's type.
+__device__ inline void store4_as(const MxMatmulArgs &a, uint32_t dtype, uint64_t row, uint64_t col, f32x4 v, bool vec)
 {
+    if (dtype == DT_F32) store4(static_cast<float *>(a.out), a.ld, row, col, a.n, v, vec);
+    else if (dtype == DT_BF16) store4(static_cast<__bf16 *>(a.out), a.ld, row, col, a.n, v, vec);
+    else store4(static_cast<_Float16 *>(a.out), a.ld, row, col, a.n, v, vec);
+}
+
+constexpr int SKINNY_WAVES = 8;
+constexpr uint32_t SKINNY_MAX_STEPS = 8;   // steps of k a wave holds A's operands of
+
+// Up to 16 MT rows of A: bound by reading B once.  The eight waves of a
+// workgroup share out k, S steps each, and hold A's operands of their steps in
+// registers; the workgroup goes through tiles of 16 rows of B.  A wave reads
+// its part of a tile along the rows (neighbouring lanes in one 64-byte piece;
+// read in the operands' order every lane's 16 bytes cost a cycle of the compute
+// unit's port, and 48 x 16384 x 5120 took 38 us), AHEAD tiles ahead, turns it
+// round through LDS, and the waves' sums are joined there in their order.
+template <int MT, int S, int AHEAD>
+__global__ __launch_bounds__(64 * SKINNY_WAVES) void k_mx_skinny(MxMatmulArgs a, uint32_t dtype, bool vec, uint32_t tiles)
+{
+    constexpr int WORDS = (S + 3) / 4;   // a lane reads the scales of a row for every fourth step
+    __shared__ __align__(16) uint8_t turned[SKINNY_WAVES][S * 1024 + WORDS * 256];
     __shared__ f32x4 sums[SKINNY_WAVES][MT][64];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const uint32_t r = lane & 15u, g = lane >> 4;
-    const uint32_t steps = (uint32_t)mx_steps(a.k);
+    const uint32_t steps = (uint32_t)mx_steps(a.k), s0 = wave * S;
+    const uint32_t mine = s0 < steps ? (steps - s0 < S ? steps - s0 : S) : 0u;   // of them there are
     const uint64_t cb = mx_code_bytes(a.k), sb = mx_scale_bytes(a.k);
-    const uint64_t n0 = (uint64_t)blockIdx.x * 16u;
-    const uint64_t row = n0 + r < a.n ? n0 + r : a.n - 1;
-    const uint8_t *bp = a.b + row * cb + g * 16u, *bsp = a.bs + row * sb;
-    const uint8_t *ap[MT], *asp[MT];
+
+    auto step = [&](uint32_t j) { return s0 + j < steps ? s0 + j : steps - 1; };
+    struct Tile {
+        u32x4 v[S];
+        uint32_t s[WORDS];
+    } w[AHEAD];
+    auto read = [&](Tile &to, uint32_t tile) {   // past the last tile: that one again, so that no branch is about a read
+        const uint64_t first = (uint64_t)(tile < tiles ? tile : tiles - 1) * 16u;
+        const uint64_t row = first + lane / 4 < a.n ? first + lane / 4 : a.n - 1, srow = first + r < a.n ? first + r : a.n - 1;
+        const uint8_t *p = a.b + row * cb + lane % 4 * 16u, *q = a.bs + srow * sb;
 #pragma unroll
-    for (int t = 0; t < MT; t++) {
-        const uint64_t m = (uint64_t)t * 16u + r < a.m ? (uint64_t)t * 16u + r : a.m - 1;
-        ap[t] = a.a + m * cb + g * 16u;
-        asp[t] = a.as + m * sb;
-    }
-    const uint32_t per = (steps + SKINNY_WAVES - 1) / SKINNY_WAVES;
-    const uint32_t s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
-    f32x4 acc[MT] = {};
-    const uint32_t sh = g * 8u;
-    for (uint32_t s = s0; s < s1; s++) {
-        const u32x4 b = *reinterpret_cast<const u32x4 *>(bp + (uint64_t)s * 64u);
-        const uint32_t bs = *reinterpret_cast<const uint32_t *>(bsp + (uint64_t)s * 4u) >> sh;
+        for (int j = 0; j < S; j++) to.v[j] = *reinterpret_cast<const u32x4 *>(p + (uint64_t)step(j) * 64u);
+#pragma unroll
+        for (int j = 0; j < WORDS; j++) to.s[j] = *reinterpret_cast<const uint32_t *>(q + (uint64_t)step(j * 4 + g) * 4u);
+    };
+    u32x4 x[MT][S];
+    uint32_t xs[MT][S];
+    if (steps) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; d++) read(w[d], blockIdx.x + d * gridDim.x);
 #pragma unroll
         for (int t = 0; t < MT; t++) {
-            const u32x4 x = *reinterpret_cast<const u32x4 *>(ap[t] + (uint64_t)s * 64u);
-            const uint32_t xs = *reinterpret_cast<const uint32_t *>(asp[t] + (uint64_t)s * 4u) >> sh;
-            acc[t] = mfma_mx(b, bs, x, xs, acc[t]);
+            const uint64_t m = (uint64_t)t * 16u + r < a.m ? (uint64_t)t * 16u + r : a.m - 1;
+#pragma unroll
+            for (int j = 0; j < S; j++) {
+                x[t][j] = *reinterpret_cast<const u32x4 *>(a.a + m * cb + (uint64_t)step(j) * 64u + g * 16u);
+                xs[t][j] = a.as[m * sb + (uint64_t)step(j) * 4u + g];
+            }
         }
     }
+    auto tile_of = [&](Tile &b, uint32_t tile) {
+        uint8_t *lds = turned[wave];
+        f32x4 acc[MT] = {};
+        if (steps) {
 #pragma unroll
-    for (int t = 0; t < MT; t++) sums[wave][t][lane] = acc[t];
-    __syncthreads();
-    if (threadIdx.x < 64 * MT) {
-        const uint32_t t = threadIdx.x >> 6;
-        f32x4 v = sums[0][t][lane];
+            for (int j = 0; j < S; j++)
+                *reinterpret_cast<u32x4 *>(lds + j * 1024u + lane / 4 * 64u + ((lane % 4) ^ (lane / 16)) * 16u) = b.v[j];
 #pragma unroll
-        for (int w = 1; w < SKINNY_WAVES; w++) v += sums[w][t][lane];
-        const uint64_t m = (uint64_t)t * 16u + r;
-        if (m < a.m) store4(static_cast<T *>(a.out), a.ld, m, n0 + g * 4u, a.n, v, vec);
+            for (int j = 0; j < WORDS; j++) *reinterpret_cast<uint32_t *>(lds + S * 1024u + j * 256u + (g * 16u + r) * 4u) = b.s[j];
+            read(b, tile + AHEAD * gridDim.x);
+#pragma unroll
+            for (int j = 0; j < S; j++) {
+                if ((uint32_t)j >= mine) break;
+                const u32x4 y = *reinterpret_cast<const u32x4 *>(lds + j * 1024u + r * 64u + ((g ^ (r / 4)) * 16u));
+                const uint32_t ys = lds[S * 1024u + j / 4 * 256u + (j % 4 * 16u + r) * 4u + g];
+#pragma unroll
+                for (int t = 0; t < MT; t++) acc[t] = mfma_mx(y, ys, x[t][j], xs[t][j], acc[t]);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();   // the sums before have been read; reads under way stay so
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int t = 0; t < MT; t++) sums[wave][t][lane] = acc[t];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (wave < MT) {
+            f32x4 v = sums[0][wave][lane];
+#pragma unroll
+            for (int q = 1; q < SKINNY_WAVES; q++) v += sums[q][wave][lane];
+            const uint64_t m = (uint64_t)wave * 16u + r;
+            if (m < a.m) store4_as(a, dtype, m, (uint64_t)tile * 16u + g * 4u, v, vec);
+        }
+    };
+    for (uint32_t tile = blockIdx.x; tile < tiles;) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; d++) {
+            if (d && tile >= tiles) break;
+            tile_of(w[d], tile);
+            tile += gridDim.x;
+        }
     }
 }
 
@@ -100,154 +169,229 @@ __global__ __launch_bounds__(64 * SKINNY_WAVES) void k_mx_skinny(MxMatmulArgs a,
 typedef const __attribute__((address_space(1))) void *gptr;
 typedef __attribute__((address_space(3))) void *lptr;
 
-// A tile of BM x BN sums; WM x WN waves.  A stage is 256 values of k (128
-// bytes of codes a row, whole lines), copied from memory straight to LDS, two
-// stages in turn: the next one's copies run while this one is multiplied.
-// In LDS chunk c (16 bytes) of row r stands at chunk c ^ (r / 2 % 8) of the
-// row, so the 16 lanes that read one chunk of 16 rows meet every bank once.
-template <class T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_mx_tile(MxMatmulArgs a, uint32_t mt, uint32_t nt, bool vec)
+template <int I>
+struct Index {
+    static constexpr int value = I;
+};
+
+// A tile of BM x BN sums, 2 x WN waves of (BM / 2) x (BN / WN).  A stage is 256
+// values of k (128 bytes of codes a row), copied from memory straight to LDS,
+// BUFFERS stages in a ring.  A compute unit's port takes one 64-byte piece a
+// cycle, and a row's scales are a piece of their own: they are copied for four
+// stages at a time (32 bytes a row), a quarter of the rows with every stage
+// (a word a row and stage cost more than the codes did: 8192^3 in 345 us).
+// A stage has four
+// instruction steps; lanes of half h of a wave take its blocks 4 h ... + 3 in
+// turn, so that their scales are one word.  While a step is multiplied from
+// registers the next one is read from LDS, and a stage's last step is
+// multiplied after the next one's first is on its way.  In LDS chunk c (16
+// bytes) of row r stands at chunk c ^ (r / 2 % 8) of the row, so the 16 lanes
+// that read one chunk of 16 rows meet every bank once.
+// Two chunks of scales go with two stages of codes (LDS holds no more), three
+// with up to four.
+constexpr int scale_chunks(int buffers) { return buffers == 2 ? 2 : 3; }
+
+template <class T, int BM, int BN, int WN, int BUFFERS>
+__global__ __launch_bounds__(128 * WN) void k_mx_tile(MxMatmulArgs a, uint32_t mt, uint32_t nt, bool vec)
 {
-    constexpr int THREADS = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr int CODES = (BM + BN) * 128, SCALES = (BM + BN) * 8;
+    constexpr uint32_t THREADS = 128 * WN, PASS = THREADS / 8;   // rows of codes that the workgroup copies at a time
+    constexpr int TM = BM / 64, TN = BN / WN / 32, PA = BM / PASS, PB = BN / PASS, WORDS = 2 * (BM + BN) / THREADS, COPIES = PA + PB + WORDS;
+    constexpr uint32_t STAGE = (BM + BN) * 128, CHUNK = (BM + BN) * 32, CODES = BUFFERS * STAGE;   // codes of a stage, scales of four; all codes
+    constexpr uint32_t CHUNKS = scale_chunks(BUFFERS);
+    static_assert(BM == BN && BM % PASS == 0 && 2 * (BM + BN) % THREADS == 0, "whole passes, and quarters of one operand's rows");
     extern __shared__ __align__(16) uint8_t lds[];
-    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t r = lane & 15u, g = lane >> 4;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
+    const uint32_t r = lane & 31u, half = lane >> 5;
     // tiles are dealt so that the workgroups of one XCD (every eighth of the
     // launch) have neighbouring tiles, eight rows of tiles by column
     const uint32_t total = mt * nt, id = blockIdx.x;
-    const uint32_t q = total / 8, rest = total % 8, xcd = id % 8;
-    const uint32_t tile = xcd * q + (xcd < rest ? xcd : rest) + id / 8;
+    const uint32_t q = total / 8, left = total % 8, xcd = id % 8;
+    const uint32_t tile = xcd * q + (xcd < left ? xcd : left) + id / 8;
     constexpr uint32_t GROUP = 8;
     const uint32_t grp = tile / (GROUP * nt), first = grp * GROUP;
     const uint32_t gm = mt - first < GROUP ? mt - first : GROUP;
     const uint32_t in = tile - grp * GROUP * nt;
     const uint64_t m0 = (uint64_t)(first + in % gm) * BM, n0 = (uint64_t)(in / gm) * BN;
 
-    const uint64_t cb = mx_code_bytes(a.k), sb = mx_scale_bytes(a.k);
-    const uint32_t steps = (uint32_t)mx_steps(a.k), stages = (steps + 1) / 2;
-
-    // what this thread copies: row and chunk of each of its 16-byte pieces
-    // (A's rows first, then B's), row and word of its scales
-    constexpr int PIECES = CODES / 16 / THREADS, WORDS = (SCALES / 4 + THREADS - 1) / THREADS;
-    static_assert(CODES / 16 % THREADS == 0 && BM * 8 % THREADS == 0, "whole pieces a thread");
-    const uint8_t *src[PIECES];
-    uint32_t off[PIECES];
+    const uint32_t cb = (uint32_t)mx_code_bytes(a.k), sb = (uint32_t)mx_scale_bytes(a.k), steps = (uint32_t)mx_steps(a.k);
+    const uint32_t stages = (steps + 1) / 2;
+    // what this thread copies of a stage: a chunk of every PASS-th row of A,
+    // then of B, and words of scales; rows past the last are that one again
+    const uint8_t *ca = a.a + m0 * cb, *cn = a.b + n0 * cb, *sa = a.as + m0 * sb, *sn = a.bs + n0 * sb;
+    const uint32_t lm = (uint32_t)(a.m - m0 < BM ? a.m - m0 : BM) - 1u, ln = (uint32_t)(a.n - n0 < BN ? a.n - n0 : BN) - 1u;
+    const uint32_t chunk = ((tid % 8) ^ (tid / 16 % 8)) * 16u;
+    uint32_t offa[PA], offb[PB];
 #pragma unroll
-    for (int i = 0; i < PIECES; i++) {
-        const uint32_t piece = i * THREADS + threadIdx.x, row = piece / 8, c = (piece % 8) ^ (row / 2 % 8);
-        off[i] = c * 16u;
-        if (row < BM) {
-            const uint64_t m = m0 + row < a.m ? m0 + row : a.m - 1;
-            src[i] = a.a + m * cb;
-        } else {
-            const uint64_t n = n0 + row - BM < a.n ? n0 + row - BM : a.n - 1;
-            src[i] = a.b + n * cb;
-        }
+    for (int i = 0; i < PA; i++) {
+        const uint32_t row = i * PASS + tid / 8;
+        offa[i] = (row < lm ? row : lm) * cb + chunk;
     }
-    const uint8_t *ssrc[WORDS];
-    uint32_t soff[WORDS];
 #pragma unroll
-    for (int i = 0; i < WORDS; i++) {
-        const uint32_t w = i * THREADS + threadIdx.x, row = w / 2;
-        soff[i] = (w % 2) * 4u;
-        if (row < BM) {
-            const uint64_t m = m0 + row < a.m ? m0 + row : a.m - 1;
-            ssrc[i] = a.as + m * sb;
-        } else {
-            const uint64_t n = n0 + row - BM < a.n ? n0 + row - BM : a.n - 1;
-            ssrc[i] = a.bs + n * sb;
-        }
+    for (int i = 0; i < PB; i++) {
+        const uint32_t row = i * PASS + tid / 8;
+        offb[i] = (row < ln ? row : ln) * cb + chunk;
     }
-    auto copy = [&](uint32_t stage) {
-        uint8_t *base = lds + (stage & 1u) * (CODES + SCALES);
-        const uint32_t kb = stage * 128u, ks = stage * 8u;
-#pragma unroll
-        for (int i = 0; i < PIECES; i++) {
-            // a row may end inside the last stage: its first half is read instead (and not multiplied)
-            const uint32_t at = kb + off[i] < cb ? kb + off[i] : kb + off[i] - 64u;
-            __builtin_amdgcn_global_load_lds((gptr)(src[i] + at), (lptr)(base + (i * THREADS + wave * 64u) * 16u), 16, 0, 0);
-        }
+    // a quarter of the scales of stages 4 c ... + 3; word w of a row stands at w ^ (row / 8 % 8)
+    auto copy_scales = [&](uint32_t c, uint32_t quarter) {
+        const uint8_t *from = quarter < 2 ? sa : sn;
+        const uint32_t lim = quarter < 2 ? lm : ln;
 #pragma unroll
         for (int i = 0; i < WORDS; i++) {
-            const uint32_t at = ks + soff[i] < sb ? ks + soff[i] : ks + soff[i] - 4u;
-            if (i * THREADS + wave * 64u < SCALES / 4)
-                __builtin_amdgcn_global_load_lds((gptr)(ssrc[i] + at), (lptr)(base + CODES + (i * THREADS + wave * 64u) * 4u), 4, 0, 0);
+            const uint32_t row = quarter % 2 * (BM / 2) + (i * THREADS + tid) / 8, at = c * 32u + ((tid % 8) ^ (row / 8 % 8)) * 4u;
+            const uint32_t off = (row < lim ? row : lim) * sb + (at < sb ? at : sb - 4u);
+            __builtin_amdgcn_global_load_lds((gptr)(from + off), (lptr)(lds + CODES + c % CHUNKS * CHUNK + (quarter * (WORDS * THREADS) + i * THREADS + wave * 64u) * 4u), 4, 0, 0);
         }
     };
+    auto copy = [&](uint32_t stage) {   // past the last stage: that one again, into a buffer nobody reads
+        uint8_t *to = lds + stage % BUFFERS * STAGE;
+        const uint32_t k = stage < stages ? stage : stages - 1;
+        // a row may end after a stage's first half: that is copied twice, the second with scales of nothing
+        const uint32_t over = k * 128u + chunk >= cb ? 64u : 0u;
+#pragma unroll
+        for (int i = 0; i < PA; i++)
+            __builtin_amdgcn_global_load_lds((gptr)(ca + (offa[i] + k * 128u - over)), (lptr)(to + (i * THREADS + wave * 64u) * 16u), 16, 0, 0);
+#pragma unroll
+        for (int i = 0; i < PB; i++)
+            __builtin_amdgcn_global_load_lds((gptr)(cn + (offb[i] + k * 128u - over)), (lptr)(to + BM * 128u + (i * THREADS + wave * 64u) * 16u), 16, 0, 0);
+        // the next chunk of scales, into the place of one that nobody reads any
+        // more: with two places that is so from the stage on that is multiplied now
+        if (CHUNKS == 3) copy_scales(stage / 4 + 1, stage % 4);
+        else if (stage) copy_scales((stage - 1) / 4 + 1, (stage - 1) % 4);
+    };
 
-    const uint32_t wm = wave / WN, wn = wave % WN;
-    const uint32_t arow = wm * (BM / WM) + r, brow = BM + wn * (BN / WN) + r;
-    f32x4 acc[TM][TN] = {};
-    if (stages) copy(0);
-    for (uint32_t st = 0; st < stages; st++) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's copies of the stage have landed
-        __builtin_amdgcn_s_barrier();                      // everyone's have, and nobody reads the other buffer
-        asm volatile("" ::: "memory");
-        if (st + 1 < stages) copy(st + 1);
-        const uint8_t *base = lds + (st & 1u) * (CODES + SCALES);
-        const uint32_t subs = steps - st * 2 < 2 ? 1u : 2u;
-        for (uint32_t u = 0; u < subs; u++) {
-            u32x4 x[TM], y[TN];
-            uint32_t xs[TM], ys[TN];
+    const uint32_t wm = wave / WN * (BM / 2), wn = wave % WN * (BN / WN);
+    struct Held {
+        u32x4 x[TM], y[TN];
+    } held[2];
+    struct Scales {
+        uint32_t x[TM], y[TN];   // of this stage; of the one before, whose last step is still to be multiplied
+    } now, before;
+    const uint32_t key = r / 2 % 8;
+    auto read = [&](Held &h, uint32_t stage, uint32_t step) {
+        const uint8_t *from = lds + stage % BUFFERS * STAGE + r * 128u + (((half * 4u + step) ^ key) * 16u);
 #pragma unroll
-            for (int i = 0; i < TM; i++) {
-                const uint32_t row = arow + i * 16u;
-                x[i] = *reinterpret_cast<const u32x4 *>(base + row * 128u + (((u * 4u + g) ^ (row / 2 % 8)) * 16u));
-                xs[i] = base[CODES + row * 8u + u * 4u + g];
-            }
+        for (int i = 0; i < TN; i++) h.y[i] = *reinterpret_cast<const u32x4 *>(from + (BM + wn + i * 32u) * 128u);
 #pragma unroll
-            for (int i = 0; i < TN; i++) {
-                const uint32_t row = brow + i * 16u;
-                y[i] = *reinterpret_cast<const u32x4 *>(base + row * 128u + (((u * 4u + g) ^ (row / 2 % 8)) * 16u));
-                ys[i] = base[CODES + row * 8u + u * 4u + g];
-            }
+        for (int i = 0; i < TM; i++) h.x[i] = *reinterpret_cast<const u32x4 *>(from + (wm + i * 32u) * 128u);
+    };
+    auto read_scales = [&](Scales &to, uint32_t stage) {
+        const uint8_t *from = lds + CODES + stage / 4 % CHUNKS * CHUNK;
+        const bool none = half && stage * 2 + 1 >= steps;   // both scales 2^-127: products vanish
+        auto word = [&](uint32_t row) {
+            return none ? 0u : *reinterpret_cast<const uint32_t *>(from + row * 32u + (((stage % 4 * 2u + half) ^ (row / 8 % 8)) * 4u));
+        };
 #pragma unroll
-            for (int i = 0; i < TM; i++)
+        for (int i = 0; i < TN; i++) to.y[i] = word(BM + wn + i * 32u + r);
 #pragma unroll
-                for (int j = 0; j < TN; j++) acc[i][j] = mfma_mx(y[j], ys[j], x[i], xs[i], acc[i][j]);
+        for (int i = 0; i < TM; i++) to.x[i] = word(wm + i * 32u + r);
+    };
+    f32x16 acc[TM][TN] = {};
+    auto products = [&](auto sel, const Held &h, const Scales &s) {
+        constexpr int SEL = decltype(sel)::value;
+#pragma unroll
+        for (int i = 0; i < TM; i++)
+#pragma unroll
+            for (int j = 0; j < TN; j++) acc[i][j] = mfma_mx32<SEL>(h.y[j], s.y[j], h.x[i], s.x[i], acc[i][j]);
+    };
+    // LDS reads and products take turns
+    auto mix = [&]() {
+#pragma unroll
+        for (int i = 0; i < TM + TN; i++) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         }
+    };
+    // the stage has landed for everyone, and nobody reads the buffer that the next copy goes to
+    auto ready = [&]() {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFFERS - 2) * COPIES) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    if (stages) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; i++) copy_scales(0, i);
+#pragma unroll
+        for (uint32_t i = 0; i < BUFFERS - 1; i++) copy(i);
+        held[1] = Held{};   // nothing is left over before the first stage
+        before = Scales{};
+        for (uint32_t s = 0; s < stages; s++) {
+            ready();
+            copy(s + BUFFERS - 1);
+            read_scales(now, s);
+            read(held[0], s, 0);
+            products(Index<3>{}, held[1], before);
+            read(held[1], s, 1);
+            products(Index<0>{}, held[0], now);
+            mix();
+            read(held[0], s, 2);
+            products(Index<1>{}, held[1], now);
+            mix();
+            read(held[1], s, 3);
+            products(Index<2>{}, held[0], now);
+            mix();
+            before = now;
+        }
+        products(Index<3>{}, held[1], before);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy outlives the workgroup's LDS
     }
 #pragma unroll
     for (int i = 0; i < TM; i++) {
-        const uint64_t m = m0 + arow + i * 16u;
+        const uint64_t m = m0 + wm + i * 32u + r;
         if (m >= a.m) continue;
 #pragma unroll
         for (int j = 0; j < TN; j++)
-            store4(static_cast<T *>(a.out), a.ld, m, n0 + (brow - r - BM) + j * 16u + g * 4u, a.n, acc[i][j], vec);
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                const uint64_t n = n0 + wn + j * 32u + q * 8u + half * 4u;
+                if (n < a.n) store4(static_cast<T *>(a.out), a.ld, m, n, a.n, v, vec);
+            }
     }
 }
 
-template <class T, int MT>
-hipError_t skinny(const MxMatmulArgs &a, bool vec, hipStream_t s)
+template <int MT, int S>
+hipError_t skinny_as(const MxMatmulArgs &a, uint32_t dtype, bool vec, hipStream_t s)
 {
-    k_mx_skinny<T, MT><<<dim3((uint32_t)((a.n + 15) / 16)), 64 * SKINNY_WAVES, 0, s>>>(a, vec);
+    const uint32_t tiles = (uint32_t)((a.n + 15) / 16);
+    // one workgroup a compute unit, or two where their registers leave room
+    constexpr uint32_t most = MT * S <= 8 ? 512u : 256u;
+    constexpr int ahead = MT * S <= 16 ? 2 : 1;
+    k_mx_skinny<MT, S, ahead><<<dim3(tiles < most ? tiles : most), 64 * SKINNY_WAVES, 0, s>>>(a, dtype, vec, tiles);
     return hipGetLastError();
 }
 
-template <class T, int BM, int BN, int WM, int WN>
+template <int MT>
+hipError_t skinny_rows(const MxMatmulArgs &a, uint32_t dtype, bool vec, hipStream_t s)
+{
+    const uint32_t each = ((uint32_t)mx_steps(a.k) + SKINNY_WAVES - 1) / SKINNY_WAVES;
+    if (each <= 1) return skinny_as<MT, 1>(a, dtype, vec, s);
+    if (each <= 2) return skinny_as<MT, 2>(a, dtype, vec, s);
+    if (each <= 3) return skinny_as<MT, 3>(a, dtype, vec, s);
+    if (each <= 4) return skinny_as<MT, 4>(a, dtype, vec, s);
+    if (each <= 5) return skinny_as<MT, 5>(a, dtype, vec, s);
+    if (each <= 6) return skinny_as<MT, 6>(a, dtype, vec, s);
+    return skinny_as<MT, 8>(a, dtype, vec, s);
+}
+
+template <class T, int BM, int BN, int WN, int BUFFERS>
 hipError_t tiled(const MxMatmulArgs &a, bool vec, hipStream_t s)
 {
-    constexpr uint32_t bytes = 2 * ((BM + BN) * 128 + (BM + BN) * 8);
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_mx_tile<T, BM, BN, WM, WN>),
+    constexpr uint32_t threads = 128 * WN, bytes = (BUFFERS * 128 + scale_chunks(BUFFERS) * 32) * (BM + BN);
+    static_assert(bytes <= 160u << 10, "one workgroup's LDS");
+    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_mx_tile<T, BM, BN, WN, BUFFERS>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (once != hipSuccess) return once;
     const uint32_t mt = (uint32_t)((a.m + BM - 1) / BM), nt = (uint32_t)((a.n + BN - 1) / BN);
-    k_mx_tile<T, BM, BN, WM, WN><<<dim3(mt * nt), 64 * WM * WN, bytes, s>>>(a, mt, nt, vec);
+    k_mx_tile<T, BM, BN, WN, BUFFERS><<<dim3(mt * nt), threads, bytes, s>>>(a, mt, nt, vec);
     return hipGetLastError();
 }
 
 template <class T>
-hipError_t matmul_as(const MxMatmulArgs &a, hipStream_t s)
+hipError_t tiles_of(const MxMatmulArgs &a, bool vec, hipStream_t s)
 {
-    const bool vec = (reinterpret_cast<uintptr_t>(a.out) | (a.ld * sizeof(T))) % (4 * sizeof(T)) == 0;
-    if (a.m <= 16) return skinny<T, 1>(a, vec, s);
-    if (a.m <= 32) return skinny<T, 2>(a, vec, s);
-    if (a.m <= 48) return skinny<T, 3>(a, vec, s);
-    if (a.m <= 64) return skinny<T, 4>(a, vec, s);
     const uint64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
-    if (big >= 256) return tiled<T, 256, 256, 2, 4>(a, vec, s);
-    return tiled<T, 128, 128, 2, 2>(a, vec, s);
+    if (big >= 256) return tiled<T, 256, 256, 4, 2>(a, vec, s);
+    return tiled<T, 128, 128, 2, 4>(a, vec, s);
 }
 
 }  // namespace
@@ -256,9 +400,18 @@ size_t mx_matmul_workspace(uint64_t, uint64_t, uint64_t) { return 0; }
 
 hipError_t launch_mx_matmul(const MxMatmulArgs &a, uint32_t dtype, hipStream_t s)
 {
-    if (dtype == DT_F32) return matmul_as<float>(a, s);
-    if (dtype == DT_BF16) return matmul_as<__bf16>(a, s);
-    return matmul_as<_Float16>(a, s);
+    const size_t elem = dtype == DT_F32 ? 4 : 2;
+    const bool vec = (reinterpret_cast<uintptr_t>(a.out) | (a.ld * elem)) % (4 * elem) == 0;
+    // few rows, and k short enough for eight waves to hold their operands
+    if (a.m <= 64 && mx_steps(a.k) <= SKINNY_WAVES * SKINNY_MAX_STEPS) {
+        if (a.m <= 16) return skinny_rows<1>(a, dtype, vec, s);
+        if (a.m <= 32) return skinny_rows<2>(a, dtype, vec, s);
+        if (a.m <= 48) return skinny_rows<3>(a, dtype, vec, s);
+        return skinny_rows<4>(a, dtype, vec, s);
+    }
+    if (dtype == DT_F32) return tiles_of<float>(a, vec, s);
+    if (dtype == DT_BF16) return tiles_of<__bf16>(a, vec, s);
+    return tiles_of<_Float16>(a, vec, s);
 }
 
 }  // namespace pccl

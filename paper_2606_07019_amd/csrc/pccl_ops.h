@@ -35,6 +35,9 @@ inline __host__ __device__ uint64_t mx_scale_bytes(uint64_t cols) { return mx_st
 // extent fit 32 bits; products of two are computed in 64 bits.
 constexpr uint64_t OPS_MAX_EXTENT = 0x7FFFFFFFull;
 
+// The product's k: a tile's 256 rows of codes stay within 32-bit offsets.
+constexpr uint64_t MX_MAX_K = 1ull << 24;
+
 // The router's envelope: one wave holds a row, up to 16 logits a lane.
 constexpr uint32_t ROUTE_MAX_EXPERTS = 1024;
 constexpr uint32_t ROUTE_MAX_TOPK = 32;

@@ -178,7 +178,7 @@ pccl_status pccl_mx_matmul_workspace(pccl_ctx *c, uint64_t m, uint64_t n, uint64
     return entry(c, [&]() -> pccl_status {
         NEED(out_bytes, "out_bytes is null");
         *out_bytes = 0;
-        LIMIT(m <= OPS_MAX_EXTENT && n <= OPS_MAX_EXTENT && k <= OPS_MAX_EXTENT, "%llu x %llu x %llu (limit 2^31 - 1 each)", (ull)m, (ull)n, (ull)k);
+        LIMIT(m <= OPS_MAX_EXTENT && n <= OPS_MAX_EXTENT && k <= MX_MAX_K, "%llu x %llu x %llu (limits 2^31 - 1, 2^31 - 1, 2^24)", (ull)m, (ull)n, (ull)k);
         if (m && n) *out_bytes = mx_matmul_workspace(m, n, k);
         return PCCL_OK;
     });
@@ -190,7 +190,7 @@ pccl_status pccl_mx_matmul(pccl_ctx *c, const uint8_t *a_codes, const uint8_t *a
 {
     return entry(c, [&]() -> pccl_status {
         TRY(check_dtype(c, dtype));
-        LIMIT(k <= OPS_MAX_EXTENT, "k = %llu (limit 2^31 - 1)", (ull)k);
+        LIMIT(k <= MX_MAX_K, "k = %llu (limit 2^24)", (ull)k);
         TRY(check_rows(c, "out", out, m, n, ld, elem_bytes(dtype)));
         if (m == 0 || n == 0) return PCCL_OK;
         if (k) {

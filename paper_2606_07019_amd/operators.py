@@ -39,12 +39,19 @@ def mx_bytes(cols: int):
 
 
 class Operators:
-    """A context for the operators on one device."""
+    """A context for the operators on one device.
+
+    The smallest calls take a few microseconds on the GPU, so the way there is
+    kept short: the library's functions are called as they are, sizes of
+    workspaces are asked for once per shape, and the current stream's address
+    is taken without building a torch.cuda.Stream."""
 
     def __init__(self, device: int = 0):
         self.device = torch.device("cuda", device)
         self._index = device
         self.h = None
+        self._lib = P.load_library()
+        self._spaces = {}
         self.h = P.pccl_create(device, 0)
 
     # -- checks ------------------------------------------------------------
@@ -54,6 +61,8 @@ class Operators:
             raise ValueError(f"{name}: a matrix of {', '.join(str(t) for t in types)} on {self.device} is needed, "
                              f"got {tuple(x.shape)} {x.dtype} on {x.device}")
         rows, cols = x.shape
+        if x.is_contiguous():
+            return rows, cols, cols
         if rows == 0 or cols == 0:
             return rows, cols, cols
         if cols > 1 and x.stride(1) != 1:
@@ -61,7 +70,7 @@ class Operators:
         return rows, cols, (x.stride(0) if rows > 1 else cols)
 
     def _same(self, name, x, shape, dtype):
-        if tuple(x.shape) != shape or x.dtype != dtype or x.device != self.device or not x.is_contiguous():
+        if x.shape != shape or x.dtype != dtype or x.device != self.device or not x.is_contiguous():
             raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} on {self.device} is needed, got "
                              f"{tuple(x.shape)} {x.dtype} on {x.device}")
         return x.data_ptr()
@@ -79,29 +88,40 @@ class Operators:
         return self._same("mask", mask, (tokens,), torch.uint8)
 
     def _stream(self):
-        # the address alone: building a torch.cuda.Stream takes longer than the smallest kernels
-        return torch._C._cuda_getCurrentRawStream(self._index)
+        return torch._C._cuda_getCurrentRawStream(self._index) or None
 
-    def _empty(self, shape, dtype):
-        return torch.empty(shape, dtype=dtype, device=self.device)
+    def _empty(self, dtype, *shape):
+        return torch.empty(*shape, dtype=dtype, device=self.device)
 
-    def _space(self, nbytes):
-        return self._empty((nbytes,), torch.uint8) if nbytes else None
+    def _call(self, status):
+        if status:
+            P._check(self.h, status)
+
+    def _space(self, ask, *sizes):
+        """(workspace, its address, its size) of the call that `ask` gives the size for."""
+        nbytes = self._spaces.get((ask, sizes))
+        if nbytes is None:
+            nbytes = self._spaces[ask, sizes] = ask(self.h, *sizes)
+        if not nbytes:
+            return None, None, 0
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return ws, ws.data_ptr(), nbytes
 
     # -- microscaled 4-bit values --------------------------------------------
 
     def _pack(self, x, rows_too, cols_too):
         rows, cols, ld = self._matrix("x", x)
-        r = c = None
+        r = c = rc = rs = cc = cs = None
         if rows_too:
             cb, sb = mx_bytes(cols)
-            r = MX(self._empty((rows, cb), torch.uint8), self._empty((rows, sb), torch.uint8), cols)
+            r = MX(self._empty(torch.uint8, rows, cb), self._empty(torch.uint8, rows, sb), cols)
+            rc, rs = r.codes.data_ptr(), r.scales.data_ptr()
         if cols_too:
             cb, sb = mx_bytes(rows)
-            c = MX(self._empty((cols, cb), torch.uint8), self._empty((cols, sb), torch.uint8), rows)
-        P.pccl_mx_quantize(self.h, x.data_ptr(), _DTYPE[x.dtype], rows, cols, ld,
-                           r.codes.data_ptr() if r else None, r.scales.data_ptr() if r else None,
-                           c.codes.data_ptr() if c else None, c.scales.data_ptr() if c else None, self._stream())
+            c = MX(self._empty(torch.uint8, cols, cb), self._empty(torch.uint8, cols, sb), rows)
+            cc, cs = c.codes.data_ptr(), c.scales.data_ptr()
+        self._call(self._lib.pccl_mx_quantize(self.h, x.data_ptr(), _DTYPE[x.dtype], rows, cols, ld, rc, rs, cc, cs,
+                                              self._stream()))
         return r, c
 
     def quantize(self, x) -> MX:
@@ -120,9 +140,9 @@ class Operators:
         """The values that q stands for."""
         rows = q.codes.shape[0]
         codes, scales = self._packed("q", q, (rows,))
-        out = self._empty((rows, q.cols), dtype)
-        P.pccl_mx_dequantize(self.h, codes, scales, rows, q.cols, out.data_ptr(), _DTYPE[dtype], q.cols,
-                             self._stream())
+        out = self._empty(dtype, rows, q.cols)
+        self._call(self._lib.pccl_mx_dequantize(self.h, codes, scales, rows, q.cols, out.data_ptr(), _DTYPE[dtype],
+                                                q.cols, self._stream()))
         return out
 
     def matmul(self, a: MX, b: MX, dtype, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -133,15 +153,14 @@ class Operators:
         ac, as_ = self._packed("a", a, (m,))
         bc, bs = self._packed("b", b, (n,))
         if out is None:
-            out, ld = self._empty((m, n), dtype), n
+            out, ld = self._empty(dtype, m, n), n
         else:
             rows, cols, ld = self._matrix("out", out)
             if (rows, cols) != (m, n) or out.dtype != dtype:
                 raise ValueError(f"out: {(m, n)} of {dtype} is needed, got {(rows, cols)} of {out.dtype}")
-        nbytes = P.pccl_mx_matmul_workspace(self.h, m, n, k)
-        ws = self._space(nbytes)
-        P.pccl_mx_matmul(self.h, ac, as_, bc, bs, m, n, k, out.data_ptr(), _DTYPE[dtype], ld,
-                         ws.data_ptr() if nbytes else None, nbytes, self._stream())
+        ws, wp, nbytes = self._space(P.pccl_mx_matmul_workspace, m, n, k)
+        self._call(self._lib.pccl_mx_matmul(self.h, ac, as_, bc, bs, m, n, k, out.data_ptr(), _DTYPE[dtype], ld, wp,
+                                            nbytes, self._stream()))
         return out
 
     # -- router ----------------------------------------------------------------
@@ -149,16 +168,15 @@ class Operators:
     def route(self, logits, topk: int, normalize: bool = True, mask: Optional[torch.Tensor] = None):
         """(weights, ids, counts, order) of the topk largest logits of every row."""
         tokens, experts, ld = self._matrix("logits", logits)
-        mp = self._mask(mask, tokens)
-        nbytes = P.pccl_moe_route_workspace(self.h, tokens, experts, topk)
-        ws = self._space(nbytes)
-        weights = self._empty((tokens, topk), torch.float32)
-        ids = self._empty((tokens, topk), torch.int32)
-        counts = self._empty((experts,), torch.int32)
-        order = self._empty((tokens * topk,), torch.int32)
-        P.pccl_moe_route(self.h, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld, topk, int(normalize),
-                         mp, weights.data_ptr(), ids.data_ptr(), counts.data_ptr(), order.data_ptr(),
-                         ws.data_ptr() if nbytes else None, nbytes, self._stream())
+        mp = None if mask is None else self._mask(mask, tokens)
+        ws, wp, nbytes = self._space(P.pccl_moe_route_workspace, tokens, experts, topk)
+        weights = self._empty(torch.float32, tokens, topk)
+        ids = self._empty(torch.int32, tokens, topk)
+        counts = self._empty(torch.int32, experts)
+        order = self._empty(torch.int32, tokens * topk)
+        self._call(self._lib.pccl_moe_route(self.h, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld,
+                                            topk, normalize, mp, weights.data_ptr(), ids.data_ptr(),
+                                            counts.data_ptr(), order.data_ptr(), wp, nbytes, self._stream()))
         return weights, ids, counts, order
 
     def route_backward(self, logits, weights, ids, dweights, normalize: bool = True,
@@ -167,13 +185,12 @@ class Operators:
         tokens, experts, ld = self._matrix("logits", logits)
         topk = weights.shape[1] if weights.dim() == 2 else 0
         shape = (tokens, topk)
-        out = self._empty((tokens, experts), logits.dtype)
-        P.pccl_moe_route_backward(self.h, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld, topk,
-                                  int(normalize), self._mask(mask, tokens),
-                                  self._same("weights", weights, shape, torch.float32),
-                                  self._same("ids", ids, shape, torch.int32),
-                                  self._same("dweights", dweights, shape, torch.float32),
-                                  out.data_ptr(), experts, self._stream())
+        out = self._empty(logits.dtype, tokens, experts)
+        self._call(self._lib.pccl_moe_route_backward(
+            self.h, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld, topk, normalize,
+            None if mask is None else self._mask(mask, tokens), self._same("weights", weights, shape, torch.float32),
+            self._same("ids", ids, shape, torch.int32), self._same("dweights", dweights, shape, torch.float32),
+            out.data_ptr(), experts, self._stream()))
         return out
 
     # -- mixture-of-experts layer ------------------------------------------------
@@ -183,9 +200,10 @@ class Operators:
         """y [tokens, hidden] for x [tokens, hidden], router [experts, hidden],
         up [experts, 2 inter, hidden] (gate rows first) and down [experts,
         hidden, inter], the latter two of x's type or packed (MX)."""
+        dtype = x.dtype
         tokens, hidden, ld = self._matrix("x", x, (torch.bfloat16, torch.float16))
         experts = router.shape[0]
-        rp = self._same("router", router, (experts, hidden), x.dtype)
+        rp = self._same("router", router, (experts, hidden), dtype)
         if isinstance(up, MX) != isinstance(down, MX):
             raise ValueError("either both or neither of up and down are packed")
         if isinstance(up, MX):
@@ -196,14 +214,14 @@ class Operators:
             dp, ds = self._packed("down", down, (experts, hidden))
         else:
             inter = down.shape[-1]
-            upp, ups = self._same("up", up, (experts, 2 * inter, hidden), x.dtype), None
-            dp, ds = self._same("down", down, (experts, hidden, inter), x.dtype), None
-        nbytes = P.pccl_moe_layer_workspace(self.h, tokens, experts, topk, hidden, inter)
-        ws = self._space(nbytes)
-        y = self._empty((tokens, hidden), x.dtype)
-        P.pccl_moe_layer(self.h, x.data_ptr(), _DTYPE[x.dtype], ld, tokens, experts, topk, hidden, inter,
-                         int(normalize), self._mask(mask, tokens), rp, upp, ups, dp, ds, y.data_ptr(), hidden,
-                         ws.data_ptr() if nbytes else None, nbytes, self._stream())
+            upp, ups = self._same("up", up, (experts, 2 * inter, hidden), dtype), None
+            dp, ds = self._same("down", down, (experts, hidden, inter), dtype), None
+        ws, wp, nbytes = self._space(P.pccl_moe_layer_workspace, tokens, experts, topk, hidden, inter)
+        y = self._empty(dtype, tokens, hidden)
+        self._call(self._lib.pccl_moe_layer(
+            self.h, x.data_ptr(), _DTYPE[dtype], ld, tokens, experts, topk, hidden, inter, normalize,
+            None if mask is None else self._mask(mask, tokens), rp, upp, ups, dp, ds, y.data_ptr(), hidden, wp, nbytes,
+            self._stream()))
         return y
 
     def close(self):
