@@ -95,45 +95,55 @@ __global__ __launch_bounds__(64 * SKINNY_WAVES) void k_mx_skinny(MxMatmulArgs a,
         u32x4 v[S];
         uint32_t s[WORDS];
     } w[AHEAD];
-    auto read = [&](Tile &to, uint32_t tile) {   // past the last tile: that one again, so that no branch is about a read
-        const uint64_t first = (uint64_t)(tile < tiles ? tile : tiles - 1) * 16u;
-        const uint64_t row = first + lane / 4 < a.n ? first + lane / 4 : a.n - 1, srow = first + r < a.n ? first + r : a.n - 1;
-        const uint8_t *p = a.b + row * cb + lane % 4 * 16u, *q = a.bs + srow * sb;
+    // 16 rows from `first` on along their rows (past the last: that one again)
+    auto read = [&](Tile &to, const uint8_t *codes, const uint8_t *scales, uint64_t first, uint64_t rows) {
+        const uint64_t row = first + lane / 4 < rows ? first + lane / 4 : rows - 1, srow = first + r < rows ? first + r : rows - 1;
+        const uint8_t *p = codes + row * cb + lane % 4 * 16u, *q = scales + srow * sb;
 #pragma unroll
         for (int j = 0; j < S; j++) to.v[j] = *reinterpret_cast<const u32x4 *>(p + (uint64_t)step(j) * 64u);
 #pragma unroll
         for (int j = 0; j < WORDS; j++) to.s[j] = *reinterpret_cast<const uint32_t *>(q + (uint64_t)step(j * 4 + g) * 4u);
     };
+    // past the last tile: that one again, so that no branch is about a read
+    auto read_b = [&](Tile &to, uint32_t tile) { read(to, a.b, a.bs, (uint64_t)(tile < tiles ? tile : tiles - 1) * 16u, a.n); };
+    uint8_t *lds = turned[wave];
+    auto turn = [&](const Tile &from) {
+#pragma unroll
+        for (int j = 0; j < S; j++)
+            *reinterpret_cast<u32x4 *>(lds + j * 1024u + lane / 4 * 64u + ((lane % 4) ^ (lane / 16)) * 16u) = from.v[j];
+#pragma unroll
+        for (int j = 0; j < WORDS; j++) *reinterpret_cast<uint32_t *>(lds + S * 1024u + j * 256u + (g * 16u + r) * 4u) = from.s[j];
+    };
+    auto codes_of = [&](int j) { return *reinterpret_cast<const u32x4 *>(lds + j * 1024u + r * 64u + ((g ^ (r / 4)) * 16u)); };
+    auto scale_of = [&](int j) { return (uint32_t)lds[S * 1024u + j / 4 * 256u + (j % 4 * 16u + r) * 4u + g]; };
     u32x4 x[MT][S];
     uint32_t xs[MT][S];
     if (steps) {
+        Tile first[MT];
 #pragma unroll
-        for (int d = 0; d < AHEAD; d++) read(w[d], blockIdx.x + d * gridDim.x);
+        for (int t = 0; t < MT; t++) read(first[t], a.a, a.as, (uint64_t)t * 16u, a.m);
+#pragma unroll
+        for (int d = 0; d < AHEAD; d++) read_b(w[d], blockIdx.x + d * gridDim.x);
 #pragma unroll
         for (int t = 0; t < MT; t++) {
-            const uint64_t m = (uint64_t)t * 16u + r < a.m ? (uint64_t)t * 16u + r : a.m - 1;
+            turn(first[t]);
 #pragma unroll
             for (int j = 0; j < S; j++) {
-                x[t][j] = *reinterpret_cast<const u32x4 *>(a.a + m * cb + (uint64_t)step(j) * 64u + g * 16u);
-                xs[t][j] = a.as[m * sb + (uint64_t)step(j) * 4u + g];
+                x[t][j] = codes_of(j);
+                xs[t][j] = scale_of(j);
             }
         }
     }
     auto tile_of = [&](Tile &b, uint32_t tile) {
-        uint8_t *lds = turned[wave];
         f32x4 acc[MT] = {};
         if (steps) {
-#pragma unroll
-            for (int j = 0; j < S; j++)
-                *reinterpret_cast<u32x4 *>(lds + j * 1024u + lane / 4 * 64u + ((lane % 4) ^ (lane / 16)) * 16u) = b.v[j];
-#pragma unroll
-            for (int j = 0; j < WORDS; j++) *reinterpret_cast<uint32_t *>(lds + S * 1024u + j * 256u + (g * 16u + r) * 4u) = b.s[j];
-            read(b, tile + AHEAD * gridDim.x);
+            turn(b);
+            read_b(b, tile + AHEAD * gridDim.x);
 #pragma unroll
             for (int j = 0; j < S; j++) {
                 if ((uint32_t)j >= mine) break;
-                const u32x4 y = *reinterpret_cast<const u32x4 *>(lds + j * 1024u + r * 64u + ((g ^ (r / 4)) * 16u));
-                const uint32_t ys = lds[S * 1024u + j / 4 * 256u + (j % 4 * 16u + r) * 4u + g];
+                const u32x4 y = codes_of(j);
+                const uint32_t ys = scale_of(j);
 #pragma unroll
                 for (int t = 0; t < MT; t++) acc[t] = mfma_mx(y, ys, x[t][j], xs[t][j], acc[t]);
             }

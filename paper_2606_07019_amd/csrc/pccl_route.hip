@@ -147,27 +147,40 @@ __global__ __launch_bounds__(THREADS) void k_route_order(RouteArgs a, uint32_t g
         base[e] = SUM ? 0u : (uint32_t)a.counts[e];
         start[0][e] = 0;
     }
+    // everything that is read goes out at once: a thread's first two slots (all
+    // of them up to eight picks) and the groups' counts
+    const uint32_t slots = n * a.topk;
+    const int32_t *ids = a.ids + row0 * a.topk;
+    int32_t mine[2];
+#pragma unroll
+    for (int i = 0; i < 2; i++) mine[i] = threadIdx.x + i * THREADS < slots ? ids[threadIdx.x + i * THREADS] : -1;
+    auto slot_id = [&](uint32_t s) { return s < THREADS ? mine[0] : s < 2 * THREADS ? mine[1] : ids[s]; };
+    uint32_t all[2] = {0, 0}, before[2] = {0, 0};
+    const uint32_t quads = padded_experts(a.experts) / 4, parts = THREADS / quads, q = threadIdx.x % quads, part = threadIdx.x / quads;
+    if constexpr (SUM) {
+        const uint32_t *hist = a.hist + q;
+        for (uint32_t g = part; part < parts && g < groups; g += 16 * parts) {
+            uint32_t w[16];
+#pragma unroll
+            for (uint32_t i = 0; i < 16; i++) w[i] = g + i * parts < groups ? hist[(uint64_t)(g + i * parts) * quads] : 0u;
+#pragma unroll
+            for (uint32_t i = 0; i < 16; i++) {
+                const uint32_t even = w[i] & 0x00FF00FFu, odd = (w[i] >> 8) & 0x00FF00FFu;
+                all[0] += even;
+                all[1] += odd;
+                before[0] += g + i * parts < g0 ? even : 0u;
+                before[1] += g + i * parts < g0 ? odd : 0u;
+            }
+        }
+    }
     __syncthreads();
-    for (uint32_t s = threadIdx.x; s < n * a.topk; s += THREADS) {
-        const int32_t id = a.ids[row0 * a.topk + s];
+    for (uint32_t s = threadIdx.x; s < slots; s += THREADS) {
+        const int32_t id = slot_id(s);
         const uint32_t r = s / a.topk;
         if (id >= 0) atomicOr(&rows[r / 64][id], 1ull << (r % 64));
     }
     if constexpr (SUM) {
-        const uint32_t ep = padded_experts(a.experts), quads = ep / 4, parts = THREADS / quads;
-        const uint32_t q = threadIdx.x % quads, part = threadIdx.x / quads;
         if (part < parts) {
-            const uint32_t *hist = a.hist + q;
-            uint32_t all[2] = {0, 0}, before[2] = {0, 0};
-#pragma unroll 16
-            for (uint32_t g = part; g < groups; g += parts) {
-                const uint32_t w = hist[(uint64_t)g * quads];
-                const uint32_t even = w & 0x00FF00FFu, odd = (w >> 8) & 0x00FF00FFu;
-                all[0] += even;
-                all[1] += odd;
-                before[0] += g < g0 ? even : 0u;
-                before[1] += g < g0 ? odd : 0u;
-            }
 #pragma unroll
             for (uint32_t i = 0; i < 4; i++) {
                 const uint32_t x = q * 4 + i, sh = (i / 2) * 16;
@@ -190,10 +203,10 @@ __global__ __launch_bounds__(THREADS) void k_route_order(RouteArgs a, uint32_t g
         }
     }
     __syncthreads();
-    for (uint32_t s = threadIdx.x; s < n * a.topk; s += THREADS) {
+    for (uint32_t s = threadIdx.x; s < slots; s += THREADS) {
         const uint32_t r = s / a.topk;
         const uint64_t slot = row0 * a.topk + s;
-        const int32_t id = a.ids[slot];
+        const int32_t id = slot_id(s);
         if (id >= 0) a.order[start[r / 64][id] + (uint32_t)__popcll(rows[r / 64][id] & ((1ull << (r % 64)) - 1ull))] = (int32_t)slot;
         if (slot >= total) a.order[slot] = -1;
     }
