@@ -11,9 +11,11 @@
 // neighbouring rows, while memory wants them along a row (a compute unit's
 // port takes one 64-byte piece a cycle: read in the operands' order, 1 KiB
 // took 64 cycles and that bounded the kernels).  So a wave reads weights along
-// their rows into registers, several blocks ahead (registers hold more of what
-// is on its way than LDS could), and turns a block round through 4 KiB of LDS
-// of its own when it multiplies it.
+// their rows into registers and turns a block round through 4 KiB of LDS of its
+// own when it multiplies it.  It is the other waves of a SIMD that read in the
+// meantime: a wave that read one to four blocks ahead of its products held
+// registers that cost more waves than that gave (16 tokens and 128 experts in
+// 4 bits: the two products 177 us with none ahead, 201 with one).
 #include "pccl_topk.h"
 
 namespace pccl {
@@ -117,9 +119,11 @@ __device__ inline u32x4 row8(const uint16_t *row, uint32_t k, uint32_t end)
 // once.
 //
 // 16-bit rows: 128 bytes and two products a block; product i takes values 32 i
-// + 8 (l / 16) ... + 7.  Microscaled rows: 64 bytes, four products; a lane's
-// chunk is one group of 32 values with its scale, and product j takes its
-// values 8 j ... + 7 (both operands count k alike, so the order is free).
+// + 8 (l / 16) ... + 7.  Microscaled rows: 128 bytes, two steps of four products;
+// a lane's chunk of a step is one group of 32 values with its scale, and product
+// j takes its values 8 j ... + 7 (both operands count k alike, so the order is
+// free).  Whole 128-byte lines either way: with half lines a compute unit's
+// first-level cache had as many misses under way for half the bytes.
 
 // A matrix of one expert: rows of `len` bytes, 32-bit offsets from `base`.
 struct Rows {
@@ -135,30 +139,23 @@ struct Plain {
     struct Block {
         u32x4 v[2 * M];
     };
-    uint32_t off[2 * M], chunk[2], len;
-
-    // tile t of M rows; `apart`: rows between the M sub-tiles
+    uint32_t off[2 * M], chunk, len;
     __device__ void begin(const Rows &w, const uint32_t (&row)[M])
     {
         const uint32_t lane = threadIdx.x & 63u;
+        chunk = lane % 8 * 16u;
         len = w.len;
 #pragma unroll
-        for (uint32_t q = 0; q < 2; q++) {
-            chunk[q] = lane % 8 * 16u;
-#pragma unroll
-            for (int i = 0; i < M; i++) {
-                const uint32_t r = row[i] + q * 8u + lane / 8;
-                off[2 * i + q] = (r < w.rows ? r : w.rows - 1) * w.len;
-            }
+        for (int j = 0; j < 2 * M; j++) {
+            const uint32_t r = row[j / 2] + j % 2 * 8u + lane / 8;
+            off[j] = (r < w.rows ? r : w.rows - 1) * w.len;
         }
     }
     __device__ void read(Block &b, const Rows &w, uint32_t block, bool there) const
     {
+        const uint32_t at = block * 128u + chunk, in = at < len ? at : 0u;   // past the row's end its start is read and not used
 #pragma unroll
-        for (int j = 0; j < 2 * M; j++) {   // chunks past the row's end are read from its start and not used
-            const uint32_t at = block * 128u + chunk[j % 2], from = off[j] + (at < len ? at : 0u);
-            b.v[j] = *reinterpret_cast<const u32x4 *>(w.base + (there ? from : 0u));
-        }
+        for (int j = 0; j < 2 * M; j++) b.v[j] = *reinterpret_cast<const u32x4 *>(w.base + (there ? off[j] + in : 0u));
     }
     __device__ void turn(const Block &b, uint8_t *lds, uint32_t block) const
     {
@@ -167,7 +164,7 @@ struct Plain {
         for (int j = 0; j < 2 * M; j++) {
             const uint32_t r = j % 2 * 8u + lane / 8;
             u32x4 v = b.v[j];
-            if (block * 128u + chunk[j % 2] >= len) v = u32x4{0, 0, 0, 0};
+            if (block * 128u + chunk >= len) v = u32x4{0, 0, 0, 0};
             *reinterpret_cast<u32x4 *>(lds + j / 2 * 2048u + r * 128u + ((lane % 8) ^ (r / 2)) * 16u) = v;
         }
     }
@@ -230,50 +227,70 @@ struct Loose {
 template <int M>
 struct Micro {
     typedef __bf16 C;                    // holds every microscaled value exactly
-    static constexpr uint32_t PRODUCTS = 4, VALUES = 128, LDS = M * 1024 + 256;
-    static_assert(M <= 4, "a lane reads one word of scales a block");
+    static constexpr uint32_t PRODUCTS = 8, VALUES = 256, WORDS = (M + 1) / 2, LDS = M * 2048 + WORDS * 256;
     struct Block {
-        u32x4 v[M];
-        uint32_t s;
+        u32x4 v[2 * M];
+        uint32_t s[WORDS];
     };
-    uint32_t off[M], soff;
+    uint32_t off[2 * M], soff[WORDS], chunk, word, len, slen;
     __device__ void begin(const Rows &w, const uint32_t (&row)[M])
     {
         const uint32_t lane = threadIdx.x & 63u;
-        soff = 0;
+        chunk = lane % 8 * 16u;
+        word = lane % 2 * 4u;
+        len = w.len;
+        slen = w.slen;
 #pragma unroll
-        for (int i = 0; i < M; i++) {
-            const uint32_t r = row[i] + lane / 4, q = row[i] + lane % 16;
-            off[i] = (r < w.rows ? r : w.rows - 1) * w.len + lane % 4 * 16u;
-            if (lane / 16 == (uint32_t)i) soff = (q < w.rows ? q : w.rows - 1) * w.slen;
+        for (int j = 0; j < 2 * M; j++) {
+            const uint32_t r = row[j / 2] + j % 2 * 8u + lane / 8;
+            off[j] = (r < w.rows ? r : w.rows - 1) * w.len;
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < WORDS; j++) {   // a lane's word of scales: of sub-tile 2 j or 2 j + 1
+            const uint32_t first = lane < 32 || 2 * j + 1 >= M ? row[2 * j] : row[2 * j + 1 < M ? 2 * j + 1 : 2 * j];
+            const uint32_t r = first + lane % 32 / 2;
+            soff[j] = (r < w.rows ? r : w.rows - 1) * w.slen;
         }
     }
     __device__ void read(Block &b, const Rows &w, uint32_t block, bool there) const
     {
+        // a row may end after a block's first step: its start is read instead and not used
+        const uint32_t at = block * 128u + chunk, in = at < len ? at : 0u, sat = block * 8u + word, sin = sat < slen ? sat : 0u;
 #pragma unroll
-        for (int i = 0; i < M; i++) b.v[i] = *reinterpret_cast<const u32x4 *>(w.base + (there ? off[i] + block * 64u : 0u));
-        b.s = *reinterpret_cast<const uint32_t *>(w.scales + (there ? soff + block * 4u : 0u));
+        for (int j = 0; j < 2 * M; j++) b.v[j] = *reinterpret_cast<const u32x4 *>(w.base + (there ? off[j] + in : 0u));
+#pragma unroll
+        for (uint32_t j = 0; j < WORDS; j++) b.s[j] = *reinterpret_cast<const uint32_t *>(w.scales + (there ? soff[j] + sin : 0u));
     }
-    __device__ void turn(const Block &b, uint8_t *lds, uint32_t) const
+    __device__ void turn(const Block &b, uint8_t *lds, uint32_t block) const
     {
-        const uint32_t lane = threadIdx.x & 63u, r = lane / 4;
+        const uint32_t lane = threadIdx.x & 63u;
 #pragma unroll
-        for (int i = 0; i < M; i++) *reinterpret_cast<u32x4 *>(lds + i * 1024u + r * 64u + ((lane % 4) ^ (r / 4)) * 16u) = b.v[i];
-        reinterpret_cast<uint32_t *>(lds + M * 1024u)[lane] = b.s;
+        for (int j = 0; j < 2 * M; j++) {
+            const uint32_t r = j % 2 * 8u + lane / 8;
+            u32x4 v = b.v[j];
+            if (block * 128u + chunk >= len) v = u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4 *>(lds + j / 2 * 2048u + r * 128u + ((lane % 8) ^ (r / 2)) * 16u) = v;
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < WORDS; j++) reinterpret_cast<uint32_t *>(lds + M * 2048u)[j * 64u + lane] = b.s[j];
     }
     __device__ void operands(const uint8_t *lds, int i, uint32_t r, uint32_t g, u32x4 (&v)[PRODUCTS]) const
     {
-        const u32x4 c = *reinterpret_cast<const u32x4 *>(lds + i * 1024u + r * 64u + ((g ^ (r / 4)) * 16u));
-        const float f = mx_scale(lds[M * 1024u + (i * 16u + r) * 4u + g]);
 #pragma unroll
-        for (uint32_t p = 0; p < PRODUCTS; p++) {
-            v[p].x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[p], f, 0));
-            v[p].y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[p], f, 1));
-            v[p].z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[p], f, 2));
-            v[p].w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[p], f, 3));
+        for (uint32_t u = 0; u < 2; u++) {
+            const u32x4 c = *reinterpret_cast<const u32x4 *>(lds + i * 2048u + r * 128u + (((u * 4u + g) ^ (r / 2)) * 16u));
+            const float f = mx_scale(lds[M * 2048u + (i * 16u + r) * 8u + u * 4u + g]);
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) {
+                u32x4 &o = v[u * 4 + j];
+                o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], f, 0));
+                o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], f, 1));
+                o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], f, 2));
+                o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[j], f, 3));
+            }
         }
     }
-    static __device__ uint32_t at(uint32_t block, uint32_t g, uint32_t p) { return block * VALUES + g * 32u + p * 8u; }
+    static __device__ uint32_t at(uint32_t block, uint32_t g, uint32_t p) { return block * VALUES + p / 4 * 128u + g * 32u + p % 4 * 8u; }
     static __device__ void place(uint32_t k, uint32_t &product, uint32_t &g)
     {
         product = k / 128 * 4 + k % 32 / 8;
@@ -444,9 +461,9 @@ static_assert(MOE_MAX_TOKENS * ROUTE_MAX_TOPK < 1u << 16, "places fit 16 bits of
 // ---- gate and up ---------------------------------------------------------------------
 
 // Both kernels below: tiles of M x 16 rows of one expert in use, for all its
-// tokens, NT tiles of 16 at a time.  Where many experts may be in use a wave
-// has tiles of its own; where few are, the four waves of a workgroup SHARE a
-// tile's k and join their sums in LDS in their order.
+// tokens, NT tiles of 16 at a time.  The four waves of a workgroup SHARE a
+// tile's k and join their sums in LDS in their order, or each has tiles of its
+// own.
 struct Walk {
     uint32_t tile, tiles, by;   // this wave's tiles
     uint32_t b0, b1;            // this wave's blocks of k
@@ -471,19 +488,14 @@ __device__ inline Walk share_out(const MoeSpace &m, uint32_t wave, uint32_t tile
     return w;
 }
 
-template <int I>
-struct Index {
-    static constexpr int value = I;
-};
-
-// Runs a wave through its tiles, tokens and blocks with DEPTH blocks held or
-// on their way: read(d, at, there) starts the reads of what block `at` takes
-// into buffer d, multiply(d, at, n) makes its products, join(at, n) ends a
-// tile.  Past the end (not `there`) read makes as many reads of nothing in
-// particular: their number must not depend on a branch, or the compiler has to
-// wait for all of them where a block of several under way is used.
-template <int NT, int DEPTH, class Read, class Multiply, class Join>
-__device__ inline void walk(const Walk &w, Read read, Multiply multiply, Join join)
+// Runs a wave through its tiles, tokens and blocks: rows(at, there) starts the
+// reads of a block's rows, tokens(at) of what its products take of the tokens,
+// turn(at) brings the rows in order, multiply(at, n) makes the products,
+// join(at, n) ends a tile.  Past the end (not `there`) as many reads are made of
+// nothing in particular: their number must not depend on a branch, or the
+// compiler has to wait for all of them where some are used.
+template <int NT, class Rows, class Tokens, class Turn, class Multiply, class Join>
+__device__ inline void walk(const Walk &w, Rows rows, Tokens tokens, Turn turn, Multiply multiply, Join join)
 {
     auto next = [&](At at) {
         if (++at.b < w.b1) return at;
@@ -495,37 +507,21 @@ __device__ inline void walk(const Walk &w, Read read, Multiply multiply, Join jo
         return at;
     };
     auto count = [&](const At &at) { return w.p1 - at.p < 16 * NT ? w.p1 - at.p : 16 * NT; };
-    At q[DEPTH];
-    q[0] = At{w.tile, w.b0, w.p0};
+    At at{w.tile, w.b0, w.p0};
     if (w.b0 >= w.b1) {   // no blocks for this wave: it only joins
-        for (At at = q[0]; at.tile < w.tiles; at = next(at)) join(at, count(at));
+        for (; at.tile < w.tiles; at = next(at)) join(at, count(at));
         return;
     }
-    auto start = [&](auto at) {
-        constexpr int d = decltype(at)::value;
-        if constexpr (d < DEPTH) {
-            if constexpr (d > 0) q[d] = next(q[d - 1]);
-            read(d, q[d], q[d].tile < w.tiles);
-        }
-    };
-    // a buffer's block, then the reads of the one DEPTH further on; false at the end
-    auto turn = [&](auto at) {
-        constexpr int d = decltype(at)::value;
-        if constexpr (d < DEPTH) {
-            if (q[d].tile >= w.tiles) return false;
-            multiply(d, q[d], count(q[d]));
-            if (q[d].b + 1 == w.b1) join(q[d], count(q[d]));
-            q[d] = next(q[(d + DEPTH - 1) % DEPTH]);
-            read(d, q[d], q[d].tile < w.tiles);
-        }
-        return true;
-    };
-    static_assert(DEPTH <= 4, "buffers written out below");
-    start(Index<0>{});
-    start(Index<1>{});
-    start(Index<2>{});
-    start(Index<3>{});
-    while (turn(Index<0>{}) && turn(Index<1>{}) && turn(Index<2>{}) && turn(Index<3>{})) {
+    rows(at, at.tile < w.tiles);
+    tokens(at);
+    while (at.tile < w.tiles) {
+        const At then = next(at);
+        turn(at);
+        multiply(at, count(at));
+        if (at.b + 1 == w.b1) join(at, count(at));
+        rows(then, then.tile < w.tiles);
+        tokens(then);
+        at = then;
     }
 }
 
@@ -582,7 +578,7 @@ __device__ inline f32x4 up_products(const u32x4 (&p)[N], const u32x4 (&b)[N], f3
 }
 
 // Gate and up rows: sub-tiles 2 i and 2 i + 1 of a wave's tile.
-template <class T, class W, bool VEC, int M, int NT, int DEPTH, bool SHARE>
+template <class T, class W, bool VEC, int M, int NT, bool SHARE>
 __global__ __launch_bounds__(64 * WAVES) void k_moe_up(MoeArgs a, MoeSpace m, uint32_t len, uint32_t slen)
 {
     __shared__ __align__(16) uint8_t lds[WAVES][W::LDS];
@@ -597,8 +593,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_up(MoeArgs a, MoeSpace m, ui
     const uint64_t first = (uint64_t)e * 2u * a.inter;
     const Rows up{static_cast<const char *>(a.up) + first * len, a.up_scales + first * slen, 2u * a.inter, len, slen};
     W rows;
-    typename W::Block block[DEPTH];
-    u32x4 v[DEPTH][W::PRODUCTS];
+    typename W::Block block;
+    u32x4 v[W::PRODUCTS];
     for (uint32_t i = threadIdx.x; i < k.p1 - k.p0; i += 64 * WAVES) who[i] = m.slots[k.p0 + i];
     __syncthreads();
     // lanes without a token read the last one's values (their sums are not used)
@@ -607,7 +603,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_up(MoeArgs a, MoeSpace m, ui
     };
     const uint16_t *x = token(k.p0 + r);
     uint32_t held = k.p0, tile = NO_PLACE;   // whose rows x points to; the tile whose rows are read
-    auto read = [&](int d, const At &at, bool there) {
+    auto read_rows = [&](const At &at, bool there) {
         if (there && at.tile != tile) {
             tile = at.tile;
             uint32_t row[M];
@@ -618,22 +614,24 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_up(MoeArgs a, MoeSpace m, ui
             }
             rows.begin(up, row);
         }
+        rows.read(block, up, at.b, there);
+    };
+    auto read_tokens = [&](const At &at) {
         if (at.p != held) {
             held = at.p;
             x = token(at.p + r);
         }
-        rows.read(block[d], up, at.b, there);
-        load_tokens<W, VEC>(v[d], x, at.b, g, a.hidden);
+        load_tokens<W, VEC>(v, x, at.b, g, a.hidden);
     };
+    auto turn = [&](const At &at) { rows.turn(block, lds[wave], at.b); };
     f32x4 acc[M][NT] = {};
-    auto multiply = [&](int d, const At &at, uint32_t n) {
-        rows.turn(block[d], lds[wave], at.b);
-        clear_tokens<W, VEC>(v[d], at.b, g, a.hidden);
+    auto multiply = [&](const At &at, uint32_t n) {
+        clear_tokens<W, VEC>(v, at.b, g, a.hidden);
         u32x4 p[M][W::PRODUCTS];
 #pragma unroll
         for (int i = 0; i < M; i++) {
             rows.operands(lds[wave], i, r, g, p[i]);
-            acc[i][0] = up_products<T, C>(p[i], v[d], acc[i][0]);
+            acc[i][0] = up_products<T, C>(p[i], v, acc[i][0]);
         }
 #pragma unroll
         for (int t = 1; t < NT; t++) {
@@ -687,10 +685,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_up(MoeArgs a, MoeSpace m, ui
             }
         }
     };
-    walk<NT, DEPTH>(k, read, multiply, join);
+    walk<NT>(k, read_rows, read_tokens, turn, multiply, join);
 }
 
-template <class W, int M, int NT, int DEPTH, bool SHARE>
+template <class W, int M, int NT, bool SHARE>
 __global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, uint32_t len, uint32_t slen)
 {
     __shared__ __align__(16) uint8_t lds[WAVES][W::LDS];
@@ -698,14 +696,14 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, 
     typedef typename W::C C;
     constexpr uint32_t N = W::PRODUCTS, SPAN = M * 16;
     const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), r = lane & 15u, g = lane >> 4;
-    const Walk k = share_out<SHARE>(m, wave, (a.hidden + SPAN - 1) / SPAN, (uint32_t)(m.inner / W::VALUES));
+    const Walk k = share_out<SHARE>(m, wave, (a.hidden + SPAN - 1) / SPAN, (uint32_t)((m.inner + W::VALUES - 1) / W::VALUES));
     const uint32_t used = m.active[0], e = m.active[1 + blockIdx.y];
     if (blockIdx.y >= used) return;
     const uint64_t first = (uint64_t)e * a.hidden;
     const Rows down{static_cast<const char *>(a.down) + first * len, a.down_scales + first * slen, a.hidden, len, slen};
     W rows;
-    typename W::Block block[DEPTH];
-    u32x4 hv[DEPTH][N], lv[DEPTH][N];
+    typename W::Block block;
+    u32x4 hv[N], lv[N];
     uint32_t tile = NO_PLACE;   // the tile whose rows are read
     const uint32_t products = (uint32_t)(m.inner / 32);
     // lanes without a token read the last one's values (their sums are not used)
@@ -714,11 +712,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, 
         const uint64_t from = ((uint64_t)(k.p0 / 16 + blockIdx.y + (at.p - k.p0) / 16 + t) * products + at.b * N) * 64u + g * 16u + who;
 #pragma unroll
         for (uint32_t i = 0; i < N; i++) {
-            h[i] = reinterpret_cast<const u32x4 *>(m.hi)[from + i * 64u];
-            l[i] = reinterpret_cast<const u32x4 *>(m.lo)[from + i * 64u];
+            // a block's second step may be missing: its first is read again, and cleared
+            const uint64_t q = from + (at.b * N + i < products ? i * 64u : 0u);
+            h[i] = reinterpret_cast<const u32x4 *>(m.hi)[q];
+            l[i] = reinterpret_cast<const u32x4 *>(m.lo)[q];
         }
     };
-    auto read = [&](int d, const At &at, bool there) {
+    auto read_rows = [&](const At &at, bool there) {
         if (there && at.tile != tile) {
             tile = at.tile;
             uint32_t row[M];
@@ -726,20 +726,27 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, 
             for (int i = 0; i < M; i++) row[i] = tile * SPAN + i * 16u;
             rows.begin(down, row);
         }
-        rows.read(block[d], down, at.b, there);
-        inner(hv[d], lv[d], at, 0);
+        rows.read(block, down, at.b, there);
+    };
+    auto read_tokens = [&](const At &at) { inner(hv, lv, at, 0); };
+    auto turn = [&](const At &at) { rows.turn(block, lds[wave], at.b); };
+    auto clear = [&](u32x4 (&h)[N], u32x4 (&l)[N], const At &at) {
+        if ((at.b + 1) * N <= products) return;
+#pragma unroll
+        for (uint32_t i = 0; i < N; i++)
+            if (at.b * N + i >= products) h[i] = l[i] = u32x4{0, 0, 0, 0};
     };
     f32x4 acc[M][NT] = {}, rest[M][NT] = {};
-    auto multiply = [&](int d, const At &at, uint32_t n) {
-        rows.turn(block[d], lds[wave], at.b);
+    auto multiply = [&](const At &at, uint32_t n) {
+        clear(hv, lv, at);
         u32x4 p[M][N];
 #pragma unroll
         for (int i = 0; i < M; i++) {
             rows.operands(lds[wave], i, r, g, p[i]);
 #pragma unroll
             for (uint32_t j = 0; j < N; j++) {
-                acc[i][0] = Frag<C>::mul(p[i][j], hv[d][j], acc[i][0]);
-                rest[i][0] = Frag<C>::mul(p[i][j], lv[d][j], rest[i][0]);
+                acc[i][0] = Frag<C>::mul(p[i][j], hv[j], acc[i][0]);
+                rest[i][0] = Frag<C>::mul(p[i][j], lv[j], rest[i][0]);
             }
         }
 #pragma unroll
@@ -747,6 +754,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, 
             if (t * 16u >= n) break;
             u32x4 h[N], l[N];
             inner(h, l, at, t);
+            clear(h, l, at);
 #pragma unroll
             for (int i = 0; i < M; i++)
 #pragma unroll
@@ -795,7 +803,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, 
             }
         }
     };
-    walk<NT, DEPTH>(k, read, multiply, join);
+    walk<NT>(k, read_rows, read_tokens, turn, multiply, join);
 }
 
 // Each token's sum over its picks, in their order; zeros without any.
@@ -813,35 +821,41 @@ __global__ __launch_bounds__(256) void k_moe_sum(MoeArgs a, MoeSpace m)
     static_cast<T *>(a.y)[(uint64_t)t * a.ld_y + h] = Elem<T>::put(v);
 }
 
-// Tiles of all experts that may be in use from which on a wave has tiles of
-// its own: enough of them to keep every compute unit's waves busy.
-constexpr uint32_t OWN_TILES = 1u << 30;
+// Whether each wave has tiles of its own rather than a quarter of the blocks of
+// a workgroup's: where a quarter is less than four blocks, so that rounding up
+// leaves waves without work, and the tiles of the experts in use (at most
+// `most`) are enough to keep every compute unit's waves busy all the same.
+// 1536 inner values in 4 bits are six blocks: 80 us shared, 66 us this way;
+// 4096 in 4 bits are 16: 98 us shared, 110 us this way.
+inline bool own_tiles(uint64_t blocks, uint64_t tiles, uint64_t most) { return blocks < 4 * WAVES && tiles * most >= 2048; }
 
-template <class T, class WU, class WD, bool VEC, int MU, int MD, int DU, int DD, int NT>
+template <class T, class W, bool VEC, int NT>
 hipError_t experts_as(const MoeArgs &a, const MoeSpace &m, hipStream_t s)
 {
+    constexpr int M = 2;
     const uint64_t places = (uint64_t)a.tokens * a.topk;
     const uint32_t most = places < a.experts ? (uint32_t)places : a.experts;
     const bool mx = a.up_scales != nullptr;
     const uint32_t ul = mx ? (uint32_t)mx_code_bytes(a.hidden) : a.hidden * 2u, us = mx ? (uint32_t)mx_scale_bytes(a.hidden) : 0u;
     const uint32_t dl = mx ? (uint32_t)mx_code_bytes(a.inter) : a.inter * 2u, ds = mx ? (uint32_t)mx_scale_bytes(a.inter) : 0u;
-    const uint32_t up = (uint32_t)((m.inner + MU * 8 - 1) / (MU * 8)), down = (a.hidden + MD * 16 - 1) / (MD * 16);
-    if ((uint64_t)up * most < OWN_TILES) k_moe_up<T, WU, VEC, MU, NT, DU, true><<<dim3(up, most), 64 * WAVES, 0, s>>>(a, m, ul, us);
-    else k_moe_up<T, WU, VEC, MU, NT, DU, false><<<dim3((up + WAVES - 1) / WAVES, most), 64 * WAVES, 0, s>>>(a, m, ul, us);
-    if ((uint64_t)down * most < OWN_TILES) k_moe_down<WD, MD, NT, DD, true><<<dim3(down, most), 64 * WAVES, 0, s>>>(a, m, dl, ds);
-    else k_moe_down<WD, MD, NT, DD, false><<<dim3((down + WAVES - 1) / WAVES, most), 64 * WAVES, 0, s>>>(a, m, dl, ds);
+    const uint32_t up = (uint32_t)((m.inner + M * 8 - 1) / (M * 8)), down = (a.hidden + M * 16 - 1) / (M * 16);
+    auto groups = [&](uint32_t tiles, bool own) { return dim3(own ? (tiles + WAVES - 1) / WAVES : tiles, most); };
+    if (own_tiles((a.hidden + W::VALUES - 1) / W::VALUES, up, most)) k_moe_up<T, W, VEC, M, NT, false><<<groups(up, true), 64 * WAVES, 0, s>>>(a, m, ul, us);
+    else k_moe_up<T, W, VEC, M, NT, true><<<groups(up, false), 64 * WAVES, 0, s>>>(a, m, ul, us);
+    if (own_tiles((m.inner + W::VALUES - 1) / W::VALUES, down, most)) k_moe_down<W, M, NT, false><<<groups(down, true), 64 * WAVES, 0, s>>>(a, m, dl, ds);
+    else k_moe_down<W, M, NT, true><<<groups(down, false), 64 * WAVES, 0, s>>>(a, m, dl, ds);
     k_moe_sum<T><<<dim3((a.hidden + 255) / 256, a.tokens), 256, 0, s>>>(a, m);
     return hipGetLastError();
 }
 
 // Tiles of 16 tokens that share one reading of the weights: one where experts
 // have eight tokens on average at most (few have more than 16, and theirs are
-// read again), four otherwise, at the price of registers for reads ahead.
-template <class T, class WU, class WD, bool VEC, int MU, int MD, int DU, int DD>
+// read again), four otherwise, at the price of registers.
+template <class T, class W, bool VEC>
 hipError_t experts_of(const MoeArgs &a, const MoeSpace &m, hipStream_t s)
 {
-    if (a.tokens <= 16 || (uint64_t)a.tokens * a.topk <= 8ull * a.experts) return experts_as<T, WU, WD, VEC, MU, MD, DU, DD, 1>(a, m, s);
-    return experts_as<T, WU, WD, VEC, MU, MD, 2, 2, 4>(a, m, s);
+    if (a.tokens <= 16 || (uint64_t)a.tokens * a.topk <= 8ull * a.experts) return experts_as<T, W, VEC, 1>(a, m, s);
+    return experts_as<T, W, VEC, 4>(a, m, s);
 }
 
 template <int LANES, int V>
@@ -878,12 +892,9 @@ hipError_t moe_as(const MoeArgs &a, hipStream_t s)
     const bool vx = aligned(a.x) && a.ld_x % 8 == 0 && a.hidden % 8 == 0;
     const hipError_t e = picks<T>(a, m, vx && aligned(a.router), s);
     if (e != hipSuccess) return e;
-    if (a.up_scales) {
-        if (vx) return experts_of<T, Micro<4>, Micro<4>, true, 4, 4, 3, 2>(a, m, s);
-        return experts_of<T, Micro<4>, Micro<4>, false, 4, 4, 2, 2>(a, m, s);
-    }
-    if (vx && aligned(a.up) && aligned(a.down) && a.inter % 8 == 0) return experts_of<T, Plain<T, 2>, Plain<T, 2>, true, 2, 2, 3, 3>(a, m, s);
-    return experts_of<T, Loose<T, 2>, Loose<T, 2>, false, 2, 2, 2, 2>(a, m, s);
+    if (a.up_scales) return vx ? experts_of<T, Micro<2>, true>(a, m, s) : experts_of<T, Micro<2>, false>(a, m, s);
+    if (vx && aligned(a.up) && aligned(a.down) && a.inter % 8 == 0) return experts_of<T, Plain<T, 2>, true>(a, m, s);
+    return experts_of<T, Loose<T, 2>, false>(a, m, s);
 }
 
 }  // namespace

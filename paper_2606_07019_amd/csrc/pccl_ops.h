@@ -136,29 +136,6 @@ struct Elem<_Float16> {
     static __device__ _Float16 put(float v) { return (_Float16)v; }
 };
 
-// Reductions over a wave by lane exchange; every lane gets the result.
-__device__ inline float wave_max(float v)
-{
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ inline float wave_sum(float v)
-{
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-__device__ inline uint32_t wave_max(uint32_t v)
-{
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        const uint32_t w = (uint32_t)__shfl_xor((int)v, o);
-        v = w > v ? w : v;
-    }
-    return v;
-}
-
 // The scale byte as the float 2^(byte - 127) whose exponent the conversion
 // instructions read; NaN for 255.
 __device__ inline float mx_scale(uint32_t byte)
