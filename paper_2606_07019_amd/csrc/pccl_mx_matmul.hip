@@ -202,7 +202,7 @@ struct Index {
 constexpr int scale_chunks(int buffers) { return buffers == 2 ? 2 : 3; }
 
 template <class T, int BM, int BN, int WN, int BUFFERS>
-__global__ __launch_bounds__(128 * WN) void k_mx_tile(MxMatmulArgs a, uint32_t mt, uint32_t nt, bool vec)
+__global__ __launch_bounds__(128 * WN) void k_mx_tile(MxMatmulArgs a, uint32_t mt, uint32_t nt, uint32_t per, bool vec)
 {
     constexpr uint32_t THREADS = 128 * WN, PASS = THREADS / 8;   // rows of codes that the workgroup copies at a time
     constexpr int TM = BM / 64, TN = BN / WN / 32, PA = BM / PASS, PB = BN / PASS, WORDS = 2 * (BM + BN) / THREADS, COPIES = PA + PB + WORDS;
@@ -224,7 +224,8 @@ __global__ __launch_bounds__(128 * WN) void k_mx_tile(MxMatmulArgs a, uint32_t m
     const uint64_t m0 = (uint64_t)(first + in % gm) * BM, n0 = (uint64_t)(in / gm) * BN;
 
     const uint32_t cb = (uint32_t)mx_code_bytes(a.k), sb = (uint32_t)mx_scale_bytes(a.k), steps = (uint32_t)mx_steps(a.k);
-    const uint32_t stages = (steps + 1) / 2;
+    // this workgroup's stages: `stages` of them from s0 on, a multiple of four
+    const uint32_t s0 = blockIdx.y * per, all = (steps + 1) / 2, stages = all - s0 < per ? all - s0 : per;
     // what this thread copies of a stage: a chunk of every PASS-th row of A,
     // then of B, and words of scales; rows past the last are that one again
     const uint8_t *ca = a.a + m0 * cb, *cn = a.b + n0 * cb, *sa = a.as + m0 * sb, *sn = a.bs + n0 * sb;
@@ -247,14 +248,14 @@ __global__ __launch_bounds__(128 * WN) void k_mx_tile(MxMatmulArgs a, uint32_t m
         const uint32_t lim = quarter < 2 ? lm : ln;
 #pragma unroll
         for (int i = 0; i < WORDS; i++) {
-            const uint32_t row = quarter % 2 * (BM / 2) + (i * THREADS + tid) / 8, at = c * 32u + ((tid % 8) ^ (row / 8 % 8)) * 4u;
+            const uint32_t row = quarter % 2 * (BM / 2) + (i * THREADS + tid) / 8, at = (s0 / 4 + c) * 32u + ((tid % 8) ^ (row / 8 % 8)) * 4u;
             const uint32_t off = (row < lim ? row : lim) * sb + (at < sb ? at : sb - 4u);
             __builtin_amdgcn_global_load_lds((gptr)(from + off), (lptr)(lds + CODES + c % CHUNKS * CHUNK + (quarter * (WORDS * THREADS) + i * THREADS + wave * 64u) * 4u), 4, 0, 0);
         }
     };
     auto copy = [&](uint32_t stage) {   // past the last stage: that one again, into a buffer nobody reads
         uint8_t *to = lds + stage % BUFFERS * STAGE;
-        const uint32_t k = stage < stages ? stage : stages - 1;
+        const uint32_t k = s0 + (stage < stages ? stage : stages - 1);
         // a row may end after a stage's first half: that is copied twice, the second with scales of nothing
         const uint32_t over = k * 128u + chunk >= cb ? 64u : 0u;
 #pragma unroll
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(128 * WN) void k_mx_tile(MxMatmulArgs a, uint32_t m
     };
     auto read_scales = [&](Scales &to, uint32_t stage) {
         const uint8_t *from = lds + CODES + stage / 4 % CHUNKS * CHUNK;
-        const bool none = half && stage * 2 + 1 >= steps;   // both scales 2^-127: products vanish
+        const bool none = half && (s0 + stage) * 2 + 1 >= steps;   // both scales 2^-127: products vanish
         auto word = [&](uint32_t row) {
             return none ? 0u : *reinterpret_cast<const uint32_t *>(from + row * 32u + (((stage % 4 * 2u + half) ^ (row / 8 % 8)) * 4u));
         };
@@ -295,6 +296,7 @@ __global__ __launch_bounds__(128 * WN) void k_mx_tile(MxMatmulArgs a, uint32_t m
 #pragma unroll
         for (int i = 0; i < TM; i++) to.x[i] = word(wm + i * 32u + r);
     };
+    T *out = static_cast<T *>(a.out) + (uint64_t)blockIdx.y * a.m * a.ld;
     f32x16 acc[TM][TN] = {};
     auto products = [&](auto sel, const Held &h, const Scales &s) {
         constexpr int SEL = decltype(sel)::value;
@@ -354,9 +356,22 @@ __global__ __launch_bounds__(128 * WN) void k_mx_tile(MxMatmulArgs a, uint32_t m
             for (int q = 0; q < 4; q++) {
                 const f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
                 const uint64_t n = n0 + wn + j * 32u + q * 8u + half * 4u;
-                if (n < a.n) store4(static_cast<T *>(a.out), a.ld, m, n, a.n, v, vec);
+                if (n < a.n) store4(out, a.ld, m, n, a.n, v, vec);
             }
     }
+}
+
+// The sums of a shared-out k, joined in the order of its parts: a thread takes
+// four columns of a row.  Rows of the parts are padded to `ld`, whole fours.
+template <class T>
+__global__ __launch_bounds__(256) void k_mx_join(const float *parts, uint32_t splits, uint64_t m, uint64_t n, uint64_t ld, T *out, uint64_t ld_out, bool vec)
+{
+    const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x, row = i / (ld / 4), col = i % (ld / 4) * 4u;
+    if (row >= m) return;
+    const float *p = parts + row * ld + col;
+    f32x4 v = *reinterpret_cast<const f32x4 *>(p);
+    for (uint32_t j = 1; j < splits; j++) v += *reinterpret_cast<const f32x4 *>(p + (uint64_t)j * m * ld);
+    store4(out, ld_out, row, col, n, v, vec);
 }
 
 template <int MT, int S>
@@ -384,7 +399,7 @@ hipError_t skinny_rows(const MxMatmulArgs &a, uint32_t dtype, bool vec, hipStrea
 }
 
 template <class T, int BM, int BN, int WN, int BUFFERS>
-hipError_t tiled(const MxMatmulArgs &a, bool vec, hipStream_t s)
+hipError_t tiled(const MxMatmulArgs &a, uint32_t per, bool vec, hipStream_t s)
 {
     constexpr uint32_t threads = 128 * WN, bytes = (BUFFERS * 128 + scale_chunks(BUFFERS) * 32) * (BM + BN);
     static_assert(bytes <= 160u << 10, "one workgroup's LDS");
@@ -392,28 +407,65 @@ hipError_t tiled(const MxMatmulArgs &a, bool vec, hipStream_t s)
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (once != hipSuccess) return once;
     const uint32_t mt = (uint32_t)((a.m + BM - 1) / BM), nt = (uint32_t)((a.n + BN - 1) / BN);
-    k_mx_tile<T, BM, BN, WN, BUFFERS><<<dim3(mt * nt), threads, bytes, s>>>(a, mt, nt, vec);
+    const uint32_t stages = (uint32_t)(mx_steps(a.k) + 1) / 2, parts = stages ? (stages + per - 1) / per : 1;
+    k_mx_tile<T, BM, BN, WN, BUFFERS><<<dim3(mt * nt, parts), threads, bytes, s>>>(a, mt, nt, per, vec);
     return hipGetLastError();
 }
 
+// Few rows, and k short enough for eight waves to hold their operands.
+inline bool few_rows(uint64_t m, uint64_t k) { return m <= 64 && mx_steps(k) <= SKINNY_WAVES * SKINNY_MAX_STEPS; }
+
+// Stages of k that a workgroup of 128 x 128 sums takes: all, or, where such
+// tiles are too few for 256 compute units, parts of eight stages (2048 values)
+// or more, whole chunks of scales each.  16 x 4096 x 28672 takes 83 us whole and
+// 22 us in eight parts, 256 x 1024 x 8192 28 and 15; with parts of 16 stages the
+// latter takes 19, and 1000 x 1000 x 4096, where two parts gain least, 16 either way.
+constexpr uint32_t LEAST_STAGES = 8;
+inline uint32_t stages_each(uint64_t m, uint64_t n, uint64_t k)
+{
+    const uint64_t stages = (mx_steps(k) + 1) / 2, tiles = ((m + 127) / 128) * ((n + 127) / 128), want = tiles < 256 ? 256 / tiles : 1;
+    uint64_t per = (stages + want - 1) / want;
+    if (per < LEAST_STAGES) per = LEAST_STAGES;
+    per = (per + 3) / 4 * 4;
+    return (uint32_t)(per < stages ? per : stages + (stages == 0));
+}
+inline uint64_t padded(uint64_t n) { return (n + 3) / 4 * 4; }
+
+// 256 x 256 sums a workgroup where such tiles occupy every compute unit: four
+// products for two operands read from LDS.  128 x 128 otherwise, eight waves all
+// the same: two to a SIMD (2040 x 1500 x 8192 29.1 us, with four waves 30.7).
 template <class T>
 hipError_t tiles_of(const MxMatmulArgs &a, bool vec, hipStream_t s)
 {
+    const uint32_t stages = (uint32_t)(mx_steps(a.k) + 1) / 2;
     const uint64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
-    if (big >= 256) return tiled<T, 256, 256, 4, 2>(a, vec, s);
-    return tiled<T, 128, 128, 2, 4>(a, vec, s);
+    if (big >= 256) return tiled<T, 256, 256, 4, 2>(a, stages + 1, vec, s);
+    const uint32_t per = stages_each(a.m, a.n, a.k);
+    if (per >= stages) return tiled<T, 128, 128, 4, 4>(a, per, vec, s);
+    MxMatmulArgs part = a;
+    part.out = a.part;
+    part.ld = padded(a.n);
+    const hipError_t e = tiled<float, 128, 128, 4, 4>(part, per, true, s);
+    if (e != hipSuccess) return e;
+    const uint64_t threads = a.m * (part.ld / 4);
+    k_mx_join<T><<<dim3((uint32_t)((threads + 255) / 256)), 256, 0, s>>>(a.part, (stages + per - 1) / per, a.m, a.n, part.ld, static_cast<T *>(a.out), a.ld, vec);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t mx_matmul_workspace(uint64_t, uint64_t, uint64_t) { return 0; }
+size_t mx_matmul_workspace(uint64_t m, uint64_t n, uint64_t k)
+{
+    const uint64_t stages = (mx_steps(k) + 1) / 2, per = stages_each(m, n, k);
+    if (few_rows(m, k) || per >= stages) return 0;
+    return (size_t)((stages + per - 1) / per * m * padded(n) * sizeof(float));
+}
 
 hipError_t launch_mx_matmul(const MxMatmulArgs &a, uint32_t dtype, hipStream_t s)
 {
     const size_t elem = dtype == DT_F32 ? 4 : 2;
     const bool vec = (reinterpret_cast<uintptr_t>(a.out) | (a.ld * elem)) % (4 * elem) == 0;
-    // few rows, and k short enough for eight waves to hold their operands
-    if (a.m <= 64 && mx_steps(a.k) <= SKINNY_WAVES * SKINNY_MAX_STEPS) {
+    if (few_rows(a.m, a.k)) {
         if (a.m <= 16) return skinny_rows<1>(a, dtype, vec, s);
         if (a.m <= 32) return skinny_rows<2>(a, dtype, vec, s);
         if (a.m <= 48) return skinny_rows<3>(a, dtype, vec, s);

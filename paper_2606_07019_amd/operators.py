@@ -101,6 +101,8 @@ class Operators:
         """(workspace, its address, its size) of the call that `ask` gives the size for."""
         nbytes = self._spaces.get((ask, sizes))
         if nbytes is None:
+            if len(self._spaces) >= 4096:   # a caller whose sizes keep changing
+                self._spaces.clear()
             nbytes = self._spaces[ask, sizes] = ask(self.h, *sizes)
         if not nbytes:
             return None, None, 0
