@@ -263,6 +263,18 @@ def all_to_all(n_npus, members, chunk_bytes) -> Collective:
     return coll
 
 
+def all_to_all_v(n_npus, members, counts, chunk_bytes) -> Collective:
+    """counts[i][j] chunks go from member i to member j (in that order, row by
+    row); those of the diagonal stay where they are."""
+    members = list(members)
+    src_of, dests_of = [], []
+    for i, v in enumerate(members):
+        for j, u in enumerate(members):
+            src_of += [v] * int(counts[i][j])
+            dests_of += [[u]] * int(counts[i][j])
+    return collective_from_lists(n_npus, len(src_of), chunk_bytes, src_of, dests_of, [members])
+
+
 # --------------------------------------------------------------------------
 # The five benchmark-shaped workloads
 # --------------------------------------------------------------------------
