@@ -98,15 +98,22 @@ struct Frag<_Float16> {
     }
 };
 
-// Eight values from k on of a row that ends at `end`; zeros beyond it.
+// Eight values from k on of a row that ends at `end`; zeros beyond it.  VEC: the
+// row starts on 16 bytes and has whole groups of eight.  Otherwise they are read
+// at any address too, and one by one at the row's end alone (16 tokens, 32
+// experts of 2044 x 500: up and down 149 us with values one by one, 50 us so).
 template <bool VEC>
 __device__ inline u32x4 row8(const uint16_t *row, uint32_t k, uint32_t end)
 {
     if (VEC) return k < end ? *reinterpret_cast<const u32x4 *>(row + k) : u32x4{0, 0, 0, 0};
+    u32x4 v;
+    if (k + 8 <= end) {   // 16 bytes at any address
+        __builtin_memcpy(&v, row + k, 16);
+        return v;
+    }
     uint16_t t[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) t[i] = k + i < end ? row[k + i] : (uint16_t)0;
-    u32x4 v;
     __builtin_memcpy(&v, t, 16);
     return v;
 }
@@ -132,7 +139,7 @@ struct Rows {
     uint32_t rows, len, slen;
 };
 
-template <class T, int M>
+template <class T, int M, bool VEC>
 struct Plain {
     typedef T C;                         // the products' type
     static constexpr uint32_t PRODUCTS = 2, VALUES = 64, LDS = M * 2048;
@@ -154,8 +161,13 @@ struct Plain {
     __device__ void read(Block &b, const Rows &w, uint32_t block, bool there) const
     {
         const uint32_t at = block * 128u + chunk, in = at < len ? at : 0u;   // past the row's end its start is read and not used
+        if constexpr (VEC) {
 #pragma unroll
-        for (int j = 0; j < 2 * M; j++) b.v[j] = *reinterpret_cast<const u32x4 *>(w.base + (there ? off[j] + in : 0u));
+            for (int j = 0; j < 2 * M; j++) b.v[j] = *reinterpret_cast<const u32x4 *>(w.base + (there ? off[j] + in : 0u));
+        } else if (there) {   // rows that start or end anywhere
+#pragma unroll
+            for (int j = 0; j < 2 * M; j++) b.v[j] = row8<false>(reinterpret_cast<const uint16_t *>(w.base + off[j]), in / 2, len / 2);
+        }
     }
     __device__ void turn(const Block &b, uint8_t *lds, uint32_t block) const
     {
@@ -181,47 +193,6 @@ struct Plain {
         product = k / 32;
         g = k % 32 / 8;
     }
-};
-
-// The same values where rows do not start on 16 bytes: read one by one, in the operands' order.
-template <class T, int M>
-struct Loose {
-    typedef T C;
-    static constexpr uint32_t PRODUCTS = 2, VALUES = 64, LDS = M * 2048;
-    struct Block {
-        u32x4 v[2 * M];
-    };
-    uint32_t off[M];
-    __device__ void begin(const Rows &w, const uint32_t (&row)[M])
-    {
-#pragma unroll
-        for (int i = 0; i < M; i++) {
-            const uint32_t r = row[i] + (threadIdx.x & 15u);
-            off[i] = (r < w.rows ? r : w.rows - 1) * w.len;
-        }
-    }
-    __device__ void read(Block &b, const Rows &w, uint32_t block, bool there) const
-    {
-        const uint32_t g = (threadIdx.x & 63u) >> 4;
-        if (!there) return;
-#pragma unroll
-        for (int i = 0; i < M; i++)
-#pragma unroll
-            for (uint32_t p = 0; p < 2; p++)
-                b.v[2 * i + p] = row8<false>(reinterpret_cast<const uint16_t *>(w.base + off[i]), at(block, g, p), w.len / 2);
-    }
-    __device__ void turn(const Block &b, uint8_t *lds, uint32_t) const
-    {
-#pragma unroll
-        for (int j = 0; j < 2 * M; j++) reinterpret_cast<u32x4 *>(lds)[j * 64 + (threadIdx.x & 63u)] = b.v[j];
-    }
-    __device__ void operands(const uint8_t *lds, int i, uint32_t, uint32_t, u32x4 (&v)[PRODUCTS]) const
-    {
-#pragma unroll
-        for (uint32_t p = 0; p < 2; p++) v[p] = reinterpret_cast<const u32x4 *>(lds)[(2 * i + p) * 64 + (threadIdx.x & 63u)];
-    }
-    static __device__ uint32_t at(uint32_t block, uint32_t g, uint32_t p) { return Plain<T, M>::at(block, g, p); }
-    static __device__ void place(uint32_t k, uint32_t &product, uint32_t &g) { Plain<T, M>::place(k, product, g); }
 };
 
 template <int M>
@@ -893,8 +864,8 @@ hipError_t moe_as(const MoeArgs &a, hipStream_t s)
     const hipError_t e = picks<T>(a, m, vx && aligned(a.router), s);
     if (e != hipSuccess) return e;
     if (a.up_scales) return vx ? experts_of<T, Micro<2>, true>(a, m, s) : experts_of<T, Micro<2>, false>(a, m, s);
-    if (vx && aligned(a.up) && aligned(a.down) && a.inter % 8 == 0) return experts_of<T, Plain<T, 2>, true>(a, m, s);
-    return experts_of<T, Loose<T, 2>, false>(a, m, s);
+    if (vx && aligned(a.up) && aligned(a.down) && a.inter % 8 == 0) return experts_of<T, Plain<T, 2, true>, true>(a, m, s);
+    return experts_of<T, Plain<T, 2, false>, false>(a, m, s);
 }
 
 }  // namespace
