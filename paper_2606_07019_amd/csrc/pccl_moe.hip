@@ -273,7 +273,9 @@ struct Micro {
 // second holds what the first rounds away, which leaves 2^-17 of the value at
 // most with bf16.  f16 has few exponents: its first part is kept 2^8 smaller,
 // so that values up to 2^24 fit, and its second 2^11 larger than the rest is,
-// so that small values keep their digits (2^-28 is left at most).
+// so that small values keep their digits (2^-28 is left at most).  A value
+// beyond its first part's range becomes an infinity there, with nothing in the
+// second: the difference would make a NaN of it.
 template <class C>
 struct Parts;
 template <>
@@ -288,7 +290,8 @@ template <class C>
 __device__ inline void split(float v, uint16_t &hi, uint16_t &lo)
 {
     const C h = (C)(v * (1.f / Parts<C>::HI));
-    const C l = (C)((v - (float)h * Parts<C>::HI) * (1.f / Parts<C>::LO));
+    const float rest = v - (float)h * Parts<C>::HI;
+    const C l = (C)(__builtin_isinf((float)h) ? 0.f : rest * (1.f / Parts<C>::LO));
     hi = __builtin_bit_cast(uint16_t, h);
     lo = __builtin_bit_cast(uint16_t, l);
 }
@@ -833,9 +836,8 @@ template <int LANES, int V>
 hipError_t pick_as(const MoeArgs &a, const MoeSpace &m, hipStream_t s)
 {
     auto room = [](uint32_t tokens, uint32_t experts, uint32_t topk) { return (tokens + 63) / 64 * experts * 8u + experts * 4u + tokens * topk * 8u; };
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_moe_pick<LANES, V>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                       room(MOE_MAX_TOKENS, ROUTE_MAX_EXPERTS, ROUTE_MAX_TOPK));
-    if (once != hipSuccess) return once;
+    const hipError_t e = allow_lds<&k_moe_pick<LANES, V>>(room(MOE_MAX_TOKENS, ROUTE_MAX_EXPERTS, ROUTE_MAX_TOPK));
+    if (e != hipSuccess) return e;
     k_moe_pick<LANES, V><<<1, 64 * PICK_WAVES, room(a.tokens, a.experts, a.topk), s>>>(a, m);
     return hipGetLastError();
 }

@@ -424,9 +424,8 @@ hipError_t tiled(const MxMatmulArgs &a, uint32_t per, hipStream_t s)
 {
     constexpr uint32_t threads = 128 * WN, bytes = (BUFFERS * 128 + scale_chunks(BUFFERS) * 32) * (BM + BN);
     static_assert(bytes <= 160u << 10, "one workgroup's LDS");
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_mx_tile<T, BM, BN, WN, BUFFERS>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (once != hipSuccess) return once;
+    const hipError_t e = allow_lds<&k_mx_tile<T, BM, BN, WN, BUFFERS>>(bytes);
+    if (e != hipSuccess) return e;
     const uint32_t mt = (uint32_t)((a.m + BM - 1) / BM), nt = (uint32_t)((a.n + BN - 1) / BN);
     const uint32_t stages = (uint32_t)(mx_steps(a.k) + 1) / 2, parts = stages ? (stages + per - 1) / per : 1;
     k_mx_tile<T, BM, BN, WN, BUFFERS><<<dim3(mt * nt, parts), threads, bytes, s>>>(a, mt, nt, per);

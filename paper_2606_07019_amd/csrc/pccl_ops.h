@@ -3,6 +3,8 @@
 // mixture-of-experts layer (not part of the ABI).
 #pragma once
 
+#include <atomic>
+
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -116,6 +118,21 @@ size_t moe_workspace(uint32_t tokens, uint32_t experts, uint32_t topk, uint32_t 
 hipError_t launch_moe(const MoeArgs &a, uint32_t dtype, hipStream_t s);
 
 #ifdef __HIPCC__
+// Lets a kernel have `bytes` of LDS on the current device, once for each device.
+template <auto Kernel>
+inline hipError_t allow_lds(uint32_t bytes)
+{
+    static std::atomic<uint64_t> devices{0};
+    int d = 0;
+    hipError_t e = hipGetDevice(&d);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (d % 64);
+    if (d < 64 && (devices.load(std::memory_order_acquire) & bit)) return hipSuccess;
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == hipSuccess) devices.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+
 // ---- device helpers -------------------------------------------------------
 
 template <class T>

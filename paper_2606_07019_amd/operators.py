@@ -87,6 +87,11 @@ class Operators:
             mask = mask.view(torch.uint8)
         return self._same("mask", mask, (tokens,), torch.uint8)
 
+    def _type(self, dtype):
+        if dtype not in _DTYPE:
+            raise ValueError(f"one of {', '.join(str(t) for t in _DTYPE)} is needed, got {dtype}")
+        return _DTYPE[dtype]
+
     def _stream(self):
         return torch._C._cuda_getCurrentRawStream(self._index) or None
 
@@ -140,15 +145,17 @@ class Operators:
 
     def dequantize(self, q: MX, dtype) -> torch.Tensor:
         """The values that q stands for."""
+        kind = self._type(dtype)
         rows = q.codes.shape[0]
         codes, scales = self._packed("q", q, (rows,))
         out = self._empty(dtype, rows, q.cols)
-        self._call(self._lib.pccl_mx_dequantize(self.h, codes, scales, rows, q.cols, out.data_ptr(), _DTYPE[dtype],
+        self._call(self._lib.pccl_mx_dequantize(self.h, codes, scales, rows, q.cols, out.data_ptr(), kind,
                                                 q.cols, self._stream()))
         return out
 
     def matmul(self, a: MX, b: MX, dtype, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """a b^T: [rows of a, rows of b]."""
+        kind = self._type(dtype)
         if a.cols != b.cols:
             raise ValueError(f"a has rows of {a.cols} values, b of {b.cols}")
         m, n, k = a.codes.shape[0], b.codes.shape[0], a.cols
@@ -161,7 +168,7 @@ class Operators:
             if (rows, cols) != (m, n) or out.dtype != dtype:
                 raise ValueError(f"out: {(m, n)} of {dtype} is needed, got {(rows, cols)} of {out.dtype}")
         ws, wp, nbytes = self._space(P.pccl_mx_matmul_workspace, m, n, k)
-        self._call(self._lib.pccl_mx_matmul(self.h, ac, as_, bc, bs, m, n, k, out.data_ptr(), _DTYPE[dtype], ld, wp,
+        self._call(self._lib.pccl_mx_matmul(self.h, ac, as_, bc, bs, m, n, k, out.data_ptr(), kind, ld, wp,
                                             nbytes, self._stream()))
         return out
 
