@@ -77,7 +77,8 @@ constexpr uint32_t SKINNY_MAX_STEPS = 8;   // steps of k a wave holds A's operan
 // its part of a tile along the rows (neighbouring lanes in one 64-byte piece;
 // read in the operands' order every lane's 16 bytes cost a cycle of the compute
 // unit's port, and 48 x 16384 x 5120 took 38 us), AHEAD tiles ahead, turns it
-// round through LDS, and the waves' sums are joined there in their order.
+// round through LDS, and the waves' sums are joined there in their order.  48 x
+// 16384 x 5120 takes 14 us (B at 3.2 TB/s), 1 x 4096 x 4096 4.6.
 template <int MT, int S, int AHEAD>
 __global__ __launch_bounds__(64 * SKINNY_WAVES) void k_mx_skinny(MxMatmulArgs a, uint32_t dtype, bool vec, uint32_t tiles)
 {
@@ -196,7 +197,8 @@ struct Index {
 // registers the next one is read from LDS, and a stage's last step is
 // multiplied after the next one's first is on its way.  In LDS chunk c (16
 // bytes) of row r stands at chunk c ^ (r / 2 % 8) of the row, so the 16 lanes
-// that read one chunk of 16 rows meet every bank once.
+// that read one chunk of 16 rows meet every bank once.  8192^3 takes 310 us by
+// itself (3.5 PFLOP/s).
 // Two chunks of scales go with two stages of codes (LDS holds no more), three
 // with up to four.
 constexpr int scale_chunks(int buffers) { return buffers == 2 ? 2 : 3; }
