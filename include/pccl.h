@@ -509,9 +509,10 @@ pccl_status pccl_moe_layer_workspace(pccl_ctx *ctx, uint32_t tokens, uint32_t ex
  *     hidden x inter; of `dtype`, or packed codes with up_scales / down_scales
  *     (both or neither NULL).  All contiguous.
  * A token without picks (masked out) gives zeros.  Sums, the softmax and the
- * inner values are kept in 32 bits or in two parts that hold as much (with
- * PCCL_F16 up to 2^24; beyond, they are infinities); y is rounded once.  Results do not depend on the other tokens' number or picks
- * beyond the order of 32-bit sums.
+ * inner values are kept in 32 bits, over the whole range of a 32-bit number;
+ * y is rounded once.  Results do not depend on the other tokens' number or
+ * picks beyond the order of 32-bit sums.  An infinity among the weights may
+ * give a NaN where the sum it enters is infinite.
  * Limits: tokens <= 256, experts <= 1024, topk <= 32, topk <= experts, hidden
  * and inter <= 2^20, hidden * inter <= 2^29.
  */

@@ -25,6 +25,7 @@ constexpr uint32_t STEP = 128;      // rows of inner values are padded to whole 
 constexpr int WAVES = 4;            // waves of a workgroup that share out k
 constexpr int PICK_WAVES = 16;
 constexpr uint32_t NO_PLACE = 0xFFFFFFFFu;
+constexpr uint32_t PARTS = 3;       // bf16 parts of an inner value
 constexpr uint32_t MAX_SPLITS = 8;  // parts of the router's product over hidden, summed up by the picking lanes
 
 // What the kernels of one call hand on, carved from the workspace.
@@ -35,8 +36,8 @@ struct MoeSpace {
     uint32_t *slots;      // [places]: token of each place, in expert order
     float *shares;        // [places]: its weight
     uint32_t *place;      // [tokens][topk]: the slot's place, NO_PLACE for an empty pick
-    uint16_t *hi, *lo;    // the inner values, in two parts: [tiles of 16 places][products][lane][8], as
-                          // the products' second operands have them
+    uint16_t *parts;      // the inner values, in three parts: [tiles of 16 places][products][PARTS][lane][8],
+                          // as the products' second operands have them
     float *outs;          // [places][hidden]: the experts' outputs, weighted
     uint64_t inner;       // padded inner size
     uint32_t splits, row; // parts of the logits, and the length of their rows
@@ -71,8 +72,7 @@ __host__ inline size_t carve(MoeSpace &m, char *base, uint32_t tokens, uint32_t 
     m.shares = (float *)take(places * 4);
     m.place = (uint32_t *)take(places * 4);
     const uint64_t tiles = places / 16 + (places < experts ? places : experts) + 1;
-    m.hi = (uint16_t *)take(tiles * 16 * m.inner * 2);
-    m.lo = (uint16_t *)take(tiles * 16 * m.inner * 2);
+    m.parts = (uint16_t *)take(tiles * 16 * m.inner * PARTS * 2);
     m.outs = (float *)take(places * hidden * 4);
     return off;
 }
@@ -269,31 +269,31 @@ struct Micro {
     }
 };
 
-// A 32-bit value in two parts of the products' type: v = hi HI + lo LO.  The
-// second holds what the first rounds away, which leaves 2^-17 of the value at
-// most with bf16.  f16 has few exponents: its first part is kept 2^8 smaller,
-// so that values up to 2^24 fit, and its second 2^11 larger than the rest is,
-// so that small values keep their digits (2^-28 is left at most).  A value
-// beyond its first part's range becomes an infinity there, with nothing in the
-// second: the difference would make a NaN of it.
-template <class C>
-struct Parts;
-template <>
-struct Parts<__bf16> {
-    static constexpr float HI = 1.f, LO = 1.f;
-};
-template <>
-struct Parts<_Float16> {
-    static constexpr float HI = 256.f, LO = 0.125f;
-};
-template <class C>
-__device__ inline void split(float v, uint16_t &hi, uint16_t &lo)
+// A 32-bit value in three parts of bf16, eight digits each: v = hi + mid + lo,
+// exactly, over the whole range (digits below 2^-133 aside).  The parts are cut
+// off and not rounded, so that each has v's sign and a finite value never gives
+// an infinity; of an infinity the first part holds all (the difference would
+// be a NaN).  An f16 value's eleven digits end within the second part.
+__device__ inline void split(float v, uint16_t &hi, uint16_t &mid, uint16_t &lo)
 {
-    const C h = (C)(v * (1.f / Parts<C>::HI));
-    const float rest = v - (float)h * Parts<C>::HI;
-    const C l = (C)(__builtin_isinf((float)h) ? 0.f : rest * (1.f / Parts<C>::LO));
-    hi = __builtin_bit_cast(uint16_t, h);
-    lo = __builtin_bit_cast(uint16_t, l);
+    const uint32_t h = __float_as_uint(v) & 0xFFFF0000u;
+    const float rest = __builtin_isinf(v) ? 0.f : v - __uint_as_float(h);
+    const uint32_t m = __float_as_uint(rest) & 0xFFFF0000u;
+    hi = (uint16_t)(h >> 16);
+    mid = (uint16_t)(m >> 16);
+    lo = (uint16_t)(__float_as_uint(rest - __uint_as_float(m)) >> 16);
+}
+
+// Eight f16 values in two operands of bf16.
+__device__ inline void split8(u32x4 v, u32x4 &hi, u32x4 &lo)
+{
+    uint16_t h[8], l[8], none;
+    _Float16 f[8];
+    __builtin_memcpy(f, &v, 16);
+#pragma unroll
+    for (int j = 0; j < 8; j++) split((float)f[j], h[j], l[j], none);
+    __builtin_memcpy(&hi, h, 16);
+    __builtin_memcpy(&lo, l, 16);
 }
 
 // A value that all lanes of a wave have alike, kept as one.
@@ -536,15 +536,9 @@ __device__ inline f32x4 up_products(const u32x4 (&p)[N], const u32x4 (&b)[N], f3
     for (uint32_t i = 0; i < N; i++) {
         if constexpr (__is_same(T, C)) {
             sum = Frag<C>::mul(p[i], b[i], sum);
-        } else {   // f16 tokens against microscaled weights: two bf16 parts hold an f16 value exactly
-            uint16_t h[8], l[8];
-            _Float16 v[8];
-            __builtin_memcpy(v, &b[i], 16);
-#pragma unroll
-            for (int j = 0; j < 8; j++) split<C>((float)v[j], h[j], l[j]);
+        } else {   // f16 tokens against microscaled weights
             u32x4 bh, bl;
-            __builtin_memcpy(&bh, h, 16);
-            __builtin_memcpy(&bl, l, 16);
+            split8(b[i], bh, bl);
             sum = Frag<C>::mul(p[i], bh, sum);
             sum = Frag<C>::mul(p[i], bl, sum);
         }
@@ -647,32 +641,38 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_up(MoeArgs a, MoeSpace m, ui
                 const uint32_t i0 = at.tile * SPAN + i * 16u + g * 4u;
                 if (i0 >= m.inner) continue;
                 const f32x4 gate = s[2 * i], lift = s[2 * i + 1];
-                uint16_t hi[4], lo[4];
+                uint16_t part[PARTS][4];
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
                     const float h = i0 + q < a.inter ? gate[q] / (1.f + expf(-gate[q])) * lift[q] : 0.f;
-                    split<C>(h, hi[q], lo[q]);
+                    split(h, part[0][q], part[1][q], part[2][q]);
                 }
                 uint32_t product, group;
                 W::place(i0, product, group);
                 const uint64_t to =
-                    (((uint64_t)(k.p0 / 16 + blockIdx.y + (at.p - k.p0) / 16 + t) * (m.inner / 32) + product) * 64u + group * 16u + r) * 8u + i0 % 8;
-                __builtin_memcpy(__builtin_assume_aligned(m.hi + to, 8), hi, 8);
-                __builtin_memcpy(__builtin_assume_aligned(m.lo + to, 8), lo, 8);
+                    (((uint64_t)(k.p0 / 16 + blockIdx.y + (at.p - k.p0) / 16 + t) * (m.inner / 32) + product) * (PARTS * 64u) + group * 16u + r) * 8u + i0 % 8;
+#pragma unroll
+                for (uint32_t q = 0; q < PARTS; q++) __builtin_memcpy(__builtin_assume_aligned(m.parts + to + q * 512u, 8), part[q], 8);
             }
         }
     };
     walk<NT>(k, read_rows, read_tokens, turn, multiply, join);
 }
 
-// Down rows, against both parts of the inner values.  The same layers: 89 us (4.1
-// TB/s) and 64 us (3.6 TB/s); rows are shorter here.
+// Down rows, against the parts of the inner values: the first part's products
+// are summed up by themselves, the others' (2^-7 of them and less) beside them.
+// An f16 weight is taken in two parts of bf16, since a 32-bit inner value passes
+// the range of f16 on either side.  The same layers: 95 us (3.9 TB/s) and 76 us
+// (3.0 TB/s); rows are shorter here, and the parts are read beside them.  Two
+// parts took 89 and 64 us and left 2^-17 of a value; three waves a SIMD, where
+// the compiler by itself settles for two, took the latter from 84 to 76.
 template <class W, int M, int NT, bool SHARE>
-__global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, uint32_t len, uint32_t slen)
+__global__ __launch_bounds__(64 * WAVES, NT == 1 ? 3 : 1) void k_moe_down(MoeArgs a, MoeSpace m, uint32_t len, uint32_t slen)
 {
     __shared__ __align__(16) uint8_t lds[WAVES][W::LDS];
     __shared__ f32x4 sums[SHARE ? WAVES : 1][M][64];
-    typedef typename W::C C;
+    typedef Frag<__bf16> F;
+    constexpr bool TWO = !__is_same(typename W::C, __bf16);
     constexpr uint32_t N = W::PRODUCTS, SPAN = M * 16;
     const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), r = lane & 15u, g = lane >> 4;
     const Walk k = share_out<SHARE>(m, wave, (a.hidden + SPAN - 1) / SPAN, (uint32_t)((m.inner + W::VALUES - 1) / W::VALUES));
@@ -682,19 +682,19 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, 
     const Rows down{static_cast<const char *>(a.down) + first * len, a.down_scales + first * slen, a.hidden, len, slen};
     W rows;
     typename W::Block block;
-    u32x4 hv[N], lv[N];
+    u32x4 v[N][PARTS];
     uint32_t tile = NO_PLACE;   // the tile whose rows are read
     const uint32_t products = (uint32_t)(m.inner / 32);
     // lanes without a token read the last one's values (their sums are not used)
-    auto inner = [&](u32x4 (&h)[N], u32x4 (&l)[N], const At &at, uint32_t t) {
+    auto inner = [&](u32x4 (&x)[N][PARTS], const At &at, uint32_t t) {
         const uint32_t n = k.p1 - at.p - t * 16u, who = r < n ? r : n - 1;
-        const uint64_t from = ((uint64_t)(k.p0 / 16 + blockIdx.y + (at.p - k.p0) / 16 + t) * products + at.b * N) * 64u + g * 16u + who;
+        const uint64_t from = ((uint64_t)(k.p0 / 16 + blockIdx.y + (at.p - k.p0) / 16 + t) * products + at.b * N) * (PARTS * 64u) + g * 16u + who;
 #pragma unroll
         for (uint32_t i = 0; i < N; i++) {
             // a block's second step may be missing: its first is read again, and cleared
-            const uint64_t q = from + (at.b * N + i < products ? i * 64u : 0u);
-            h[i] = reinterpret_cast<const u32x4 *>(m.hi)[q];
-            l[i] = reinterpret_cast<const u32x4 *>(m.lo)[q];
+            const uint64_t q = from + (at.b * N + i < products ? i * (PARTS * 64u) : 0u);
+#pragma unroll
+            for (uint32_t c = 0; c < PARTS; c++) x[i][c] = reinterpret_cast<const u32x4 *>(m.parts)[q + c * 64u];
         }
     };
     auto read_rows = [&](const At &at, bool there) {
@@ -707,40 +707,49 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, 
         }
         rows.read(block, down, at.b, there);
     };
-    auto read_tokens = [&](const At &at) { inner(hv, lv, at, 0); };
+    auto read_tokens = [&](const At &at) { inner(v, at, 0); };
     auto turn = [&](const At &at) { rows.turn(block, lds[wave], at.b); };
-    auto clear = [&](u32x4 (&h)[N], u32x4 (&l)[N], const At &at) {
+    auto clear = [&](u32x4 (&x)[N][PARTS], const At &at) {
         if ((at.b + 1) * N <= products) return;
 #pragma unroll
         for (uint32_t i = 0; i < N; i++)
-            if (at.b * N + i >= products) h[i] = l[i] = u32x4{0, 0, 0, 0};
+            if (at.b * N + i >= products)
+#pragma unroll
+                for (uint32_t c = 0; c < PARTS; c++) x[i][c] = u32x4{0, 0, 0, 0};
     };
     f32x4 acc[M][NT] = {}, rest[M][NT] = {};
+    u32x4 p[M][N], low[TWO ? M : 1][N];   // the weights, or their two parts
+    auto multiply_by = [&](const u32x4 (&x)[N][PARTS], int i, int t) {
+#pragma unroll
+        for (uint32_t j = 0; j < N; j++) {
+            acc[i][t] = F::mul(p[i][j], x[j][0], acc[i][t]);
+#pragma unroll
+            for (uint32_t c = 1; c < PARTS; c++) rest[i][t] = F::mul(p[i][j], x[j][c], rest[i][t]);
+            if constexpr (TWO) {
+#pragma unroll
+                for (uint32_t c = 0; c < PARTS; c++) rest[i][t] = F::mul(low[i][j], x[j][c], rest[i][t]);
+            }
+        }
+    };
     auto multiply = [&](const At &at, uint32_t n) {
-        clear(hv, lv, at);
-        u32x4 p[M][N];
+        clear(v, at);
 #pragma unroll
         for (int i = 0; i < M; i++) {
             rows.operands(lds[wave], i, r, g, p[i]);
+            if constexpr (TWO) {
 #pragma unroll
-            for (uint32_t j = 0; j < N; j++) {
-                acc[i][0] = Frag<C>::mul(p[i][j], hv[j], acc[i][0]);
-                rest[i][0] = Frag<C>::mul(p[i][j], lv[j], rest[i][0]);
+                for (uint32_t j = 0; j < N; j++) split8(p[i][j], p[i][j], low[i][j]);
             }
+            multiply_by(v, i, 0);
         }
 #pragma unroll
         for (int t = 1; t < NT; t++) {
             if (t * 16u >= n) break;
-            u32x4 h[N], l[N];
-            inner(h, l, at, t);
-            clear(h, l, at);
+            u32x4 x[N][PARTS];
+            inner(x, at, t);
+            clear(x, at);
 #pragma unroll
-            for (int i = 0; i < M; i++)
-#pragma unroll
-                for (uint32_t j = 0; j < N; j++) {
-                    acc[i][t] = Frag<C>::mul(p[i][j], h[j], acc[i][t]);
-                    rest[i][t] = Frag<C>::mul(p[i][j], l[j], rest[i][t]);
-                }
+            for (int i = 0; i < M; i++) multiply_by(x, i, t);
         }
     };
     auto join = [&](const At &at, uint32_t n) {
@@ -750,7 +759,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_moe_down(MoeArgs a, MoeSpace m, 
             f32x4 s[M];
 #pragma unroll
             for (int i = 0; i < M; i++) {
-                s[i] = acc[i][t] * Parts<C>::HI + rest[i][t] * Parts<C>::LO;
+                s[i] = acc[i][t] + rest[i][t];
                 acc[i][t] = rest[i][t] = f32x4{0, 0, 0, 0};
             }
             if constexpr (SHARE) {
