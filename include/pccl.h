@@ -432,7 +432,8 @@ typedef enum { PCCL_F32 = 0, PCCL_BF16 = 1, PCCL_F16 = 2 } pccl_dtype;
  * Packs x (rows x cols of `dtype`, row stride ld): its rows into codes /
  * scales, and in the same pass its columns into codes_t / scales_t (`cols`
  * rows of `rows` values: the transpose, blocked along the rows, as the
- * products of a training step contract over them).  Either pair may be NULL.
+ * products of a training step contract over them).  Either pair may be NULL,
+ * both where x has no rows or no columns.
  * b = max(floor(log2 a) - 2, -127) + 127 for a block with largest magnitude a,
  * 0 for zeros; values go to the nearest, ties to the even code, and beyond 6
  * to 6.  A block that holds a NaN or an infinity gets b = 255: all NaN.

@@ -147,8 +147,8 @@ pccl_status pccl_mx_quantize(pccl_ctx *c, const void *x, pccl_dtype dtype, uint6
     return entry(c, [&]() -> pccl_status {
         TRY(check_dtype(c, dtype));
         TRY(check_rows(c, "x", x, rows, cols, ld, elem_bytes(dtype)));
+        if (rows == 0 || cols == 0) return PCCL_OK;   // what is written is empty too, and has no address
         NEED(codes || scales || codes_t || scales_t, "no output");
-        if (rows == 0 || cols == 0) return PCCL_OK;
         if (codes || scales) TRY(check_packed(c, "rows", codes, scales));
         if (codes_t || scales_t) TRY(check_packed(c, "columns", codes_t, scales_t));
         TRY(check_grid(c, ((rows + 127) / 128) * ((cols + 127) / 128), 256));

@@ -1,0 +1,43 @@
+"""GPU: the operators on tensors without rows or columns, as an expert that got
+no tokens gives them."""
+
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+
+from test_gpu_operators import _torch, ops  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 0), (0, 33), (5, 0)])
+def test_packing_of_nothing(ops, rows, cols):   # noqa: F811
+    print(f"[operators] packing {rows}x{cols}", flush=True)
+    t = _torch()
+    for dtype in (t.float32, t.bfloat16, t.float16):
+        x = t.empty((rows, cols), dtype=dtype, device="cuda")
+        for q, n, k in ((ops.quantize(x), rows, cols), (ops.quantize_columns(x), cols, rows), *zip(ops.quantize_both(x), (rows, cols), (cols, rows))):
+            steps = -(-k // 128)
+            assert q.codes.shape == (n, steps * 64) and q.scales.shape == (n, steps * 4) and q.cols == k
+            assert ops.dequantize(q, dtype).shape == (n, k)
+
+
+def test_an_expert_without_rows(ops):   # noqa: F811
+    print("[operators] an expert without rows", flush=True)
+    t = _torch()
+    rows, up, down = (ops.quantize(t.randn(s, device="cuda")) for s in ((0, 96), (40, 96), (96, 20)))
+    gate, lift = ops.matmul(rows, up, t.float32).chunk(2, dim=1)
+    assert ops.matmul(ops.quantize(t.nn.functional.silu(gate) * lift), down, t.bfloat16).shape == (0, 96)
+
+
+def test_example_with_fewer_tokens_than_experts():
+    print("[operators] example, 3 tokens for 16 experts", flush=True)
+    spec = importlib.util.spec_from_file_location("expert_parallel", os.path.join(ROOT, "examples", "expert_parallel.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    r = example.run(tokens=3)
+    assert r["counts"].sum() == 4 * 3 * 2 and np.isfinite(r["off"])
