@@ -406,7 +406,8 @@ pccl_status pccl_get_profile(pccl_ctx *ctx, double *setup_ms, double *match_ms, 
  * no topology and may be called at any time.  Arrays are DEVICE memory on the
  * context's device unless said otherwise.  Each call queues its kernels on
  * `hip_stream` (NULL = the default stream) and returns; it allocates nothing,
- * copies nothing to the host and may be captured into a HIP graph.  A
+ * copies nothing to the host, leaves the caller's current device as it was and
+ * may be captured into a HIP graph.  A
  * workspace is the caller's, 256-byte aligned, must not be shared by calls
  * that may overlap, and needs no initial contents.  Outputs must not overlap
  * inputs.  A row stride `ld` is counted in elements and is at least the row's

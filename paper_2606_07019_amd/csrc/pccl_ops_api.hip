@@ -58,11 +58,27 @@ pccl_status entry(pccl_ctx *c, F &&body)
         if (!(cond)) return fail(c, PCCL_EUNSUPPORTED, __VA_ARGS__);   \
     } while (0)
 
-pccl_status on_device(pccl_ctx *c)
-{
-    const hipError_t e = hipSetDevice(ctx_device(c));
-    return e == hipSuccess ? PCCL_OK : fail(c, PCCL_EDEVICE, "hipSetDevice: %s", hipGetErrorString(e));
-}
+// The context's device for the launches of a call; the caller's again at its end.
+class OnDevice {
+public:
+    pccl_status enter(pccl_ctx *c)
+    {
+        int now = 0;
+        hipError_t e = hipGetDevice(&now);
+        if (e == hipSuccess && now != ctx_device(c)) {
+            e = hipSetDevice(ctx_device(c));
+            if (e == hipSuccess) before_ = now;
+        }
+        return e == hipSuccess ? PCCL_OK : fail(c, PCCL_EDEVICE, "no device: %s", hipGetErrorString(e));
+    }
+    ~OnDevice()
+    {
+        if (before_ >= 0) (void)hipSetDevice(before_);
+    }
+
+private:
+    int before_ = -1;
+};
 
 pccl_status launched(pccl_ctx *c, hipError_t e, const char *what)
 {
@@ -152,7 +168,8 @@ pccl_status pccl_mx_quantize(pccl_ctx *c, const void *x, pccl_dtype dtype, uint6
         if (codes || scales) TRY(check_packed(c, "rows", codes, scales));
         if (codes_t || scales_t) TRY(check_packed(c, "columns", codes_t, scales_t));
         TRY(check_grid(c, ((rows + 127) / 128) * ((cols + 127) / 128), 256));
-        TRY(on_device(c));
+        OnDevice device;
+        TRY(device.enter(c));
         const MxQuantizeArgs a{x, rows, cols, ld, codes, scales, codes_t, scales_t};
         return launched(c, launch_mx_quantize(a, dtype, (hipStream_t)hip_stream), "mx_quantize");
     });
@@ -167,7 +184,8 @@ pccl_status pccl_mx_dequantize(pccl_ctx *c, const uint8_t *codes, const uint8_t 
         if (rows == 0 || cols == 0) return PCCL_OK;
         TRY(check_packed(c, "input", codes, scales));
         TRY(check_grid(c, (rows * ((cols + 511) / 512) + 3) / 4, 256));
-        TRY(on_device(c));
+        OnDevice device;
+        TRY(device.enter(c));
         const MxDequantizeArgs a{codes, scales, rows, cols, ld, out};
         return launched(c, launch_mx_dequantize(a, dtype, (hipStream_t)hip_stream), "mx_dequantize");
     });
@@ -199,7 +217,8 @@ pccl_status pccl_mx_matmul(pccl_ctx *c, const uint8_t *a_codes, const uint8_t *a
         }
         TRY(check_grid(c, ((m + 127) / 128) * ((n + 15) / 16), 512));
         TRY(check_space(c, workspace, workspace_bytes, mx_matmul_workspace(m, n, k)));
-        TRY(on_device(c));
+        OnDevice device;
+        TRY(device.enter(c));
         const MxMatmulArgs a{a_codes, a_scales, b_codes, b_scales, m, n, k, ld, out, (float *)workspace};
         return launched(c, launch_mx_matmul(a, dtype, (hipStream_t)hip_stream), "mx_matmul");
     });
@@ -232,7 +251,8 @@ pccl_status pccl_moe_route(pccl_ctx *c, const void *logits, pccl_dtype dtype, ui
         }
         TRY(check_grid(c, (tokens + ROUTE_ROWS - 1) / ROUTE_ROWS, 1024));
         TRY(check_space(c, workspace, workspace_bytes, route_workspace(tokens, experts)));
-        TRY(on_device(c));
+        OnDevice device;
+        TRY(device.enter(c));
         const RouteArgs a{logits, tokens, ld, experts, topk, normalize ? 1u : 0u, token_mask, weights, ids, counts, order, (uint32_t *)workspace};
         return launched(c, launch_route(a, dtype, (hipStream_t)hip_stream), "moe_route");
     });
@@ -253,7 +273,8 @@ pccl_status pccl_moe_route_backward(pccl_ctx *c, const void *logits, pccl_dtype 
         NEED(ids && aligned(ids, 4), "ids are null or misaligned");
         NEED(dweights && aligned(dweights, 4), "dweights are null or misaligned");
         TRY(check_grid(c, (tokens + 3) / 4, 256));
-        TRY(on_device(c));
+        OnDevice device;
+        TRY(device.enter(c));
         const RouteBackwardArgs a{logits, tokens, ld, ld_d, experts, topk, normalize ? 1u : 0u, token_mask, weights, ids, dweights, dlogits};
         return launched(c, launch_route_backward(a, dtype, (hipStream_t)hip_stream), "moe_route_backward");
     });
@@ -293,7 +314,8 @@ pccl_status pccl_moe_layer(pccl_ctx *c, const void *x, pccl_dtype dtype, uint64_
         }
         if (tokens == 0) return PCCL_OK;
         TRY(check_space(c, workspace, workspace_bytes, moe_workspace(tokens, experts, topk, hidden, inter)));
-        TRY(on_device(c));
+        OnDevice device;
+        TRY(device.enter(c));
         const MoeArgs a{x, ld_x, ld_y, tokens, experts, topk, hidden, inter, normalize ? 1u : 0u, token_mask, router, up, down,
                         up_scales, down_scales, y, (char *)workspace};
         return launched(c, launch_moe(a, dtype, (hipStream_t)hip_stream), "moe_layer");

@@ -52,7 +52,8 @@ class Operators:
         self.h = None
         self._lib = P.load_library()
         self._spaces = {}
-        self.h = P.pccl_create(device, 0)
+        with torch.cuda.device(self.device):   # both calls make it the current one and leave it so
+            self.h = P.pccl_create(device, 0)
 
     # -- checks ------------------------------------------------------------
 
@@ -235,8 +236,9 @@ class Operators:
 
     def close(self):
         if self.h is not None:
-            P.pccl_destroy(self.h)
-            self.h = None
+            h, self.h = self.h, None
+            with torch.cuda.device(self.device):
+                P.pccl_destroy(h)
 
     def __del__(self):
         try:
