@@ -438,6 +438,7 @@ typedef enum { PCCL_F32 = 0, PCCL_BF16 = 1, PCCL_F16 = 2 } pccl_dtype;
  * b = max(floor(log2 a) - 2, -127) + 127 for a block with largest magnitude a,
  * 0 for zeros; values go to the nearest, ties to the even code, and beyond 6
  * to 6.  A block that holds a NaN or an infinity gets b = 255: all NaN.
+ * Limit with columns: 2^24 - 1 tiles of 128 x 128 values.
  */
 pccl_status pccl_mx_quantize(pccl_ctx *ctx, const void *x, pccl_dtype dtype, uint64_t rows, uint64_t cols,
                              uint64_t ld, uint8_t *codes, uint8_t *scales, uint8_t *codes_t,
@@ -454,9 +455,10 @@ pccl_status pccl_mx_matmul_workspace(pccl_ctx *ctx, uint64_t m, uint64_t n, uint
 /*
  * out (m x n of `dtype`, row stride ld) = A B^T for packed A (m rows of k
  * values) and B (n rows of k values), summed in 32 bits and rounded once.  k =
- * 0 gives zeros; k is at most 2^24.  A layer's forward product takes the packed rows of x and W,
+ * 0 gives zeros.  A layer's forward product takes the packed rows of x and W,
  * its input gradient those of dy and of W's columns, its weight gradient those
  * of dy's and x's columns.
+ * Limits: k <= 2^24; at most 2^23 - 1 tiles of 256 x 256 results.
  */
 pccl_status pccl_mx_matmul(pccl_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales,
                            const uint8_t *b_codes, const uint8_t *b_scales, uint64_t m, uint64_t n,
@@ -479,7 +481,8 @@ pccl_status pccl_moe_route_workspace(pccl_ctx *ctx, uint64_t tokens, uint32_t ex
  *   counts[experts]: the picks of each expert.
  *   order[tokens * topk]: the slots (token * topk + position) by expert, those
  *     of one expert ascending, then -1 for every empty pick.
- * Limits: experts <= 1024, topk <= 32, topk <= experts, tokens * topk < 2^31.
+ * Limits: experts <= 1024, topk <= 32, topk <= experts, tokens * topk < 2^31,
+ * tokens <= 64 (2^22 - 1).
  */
 pccl_status pccl_moe_route(pccl_ctx *ctx, const void *logits, pccl_dtype dtype, uint64_t tokens,
                            uint32_t experts, uint64_t ld, uint32_t topk, int normalize,

@@ -307,13 +307,23 @@ __global__ __launch_bounds__(256) void k_mx_rows(MxQuantizeArgs a, uint32_t chun
 template <class T>
 hipError_t quantize_as(const MxQuantizeArgs &a, hipStream_t s)
 {
-    const uint32_t ct = (uint32_t)((a.cols + TILE - 1) / TILE), rt = (uint32_t)((a.rows + TILE - 1) / TILE);
-    const dim3 grid(ct * rt);
     if (!a.codes_t) {
         const uint32_t chunks = (uint32_t)((a.cols + 511) / 512);
-        const uint64_t items = (a.rows + 7) / 8 * chunks;
-        k_mx_rows<T><<<dim3((uint32_t)((items + 3) / 4)), 256, 0, s>>>(a, chunks);
-    } else if (a.codes) {
+        const uint64_t most = most_blocks(256) * 4 / chunks * 8;   // rows of a launch
+        for (uint64_t r = 0; r < a.rows; r += most) {
+            MxQuantizeArgs part = a;
+            part.x = static_cast<const T *>(a.x) + r * a.ld;
+            part.rows = a.rows - r < most ? a.rows - r : most;
+            part.codes += r * mx_code_bytes(a.cols);
+            part.scales += r * mx_scale_bytes(a.cols);
+            const uint64_t items = (part.rows + 7) / 8 * chunks;
+            k_mx_rows<T><<<dim3((uint32_t)((items + 3) / 4)), 256, 0, s>>>(part, chunks);
+        }
+        return hipGetLastError();
+    }
+    const uint32_t ct = (uint32_t)((a.cols + TILE - 1) / TILE), rt = (uint32_t)((a.rows + TILE - 1) / TILE);
+    const dim3 grid(ct * rt);
+    if (a.codes) {
         k_mx_quantize<T, true><<<grid, 256, 0, s>>>(a, ct);
     } else {
         k_mx_quantize<T, false><<<grid, 256, 0, s>>>(a, ct);
@@ -369,8 +379,15 @@ hipError_t dequantize_as(const MxDequantizeArgs &a, hipStream_t s)
 {
     const bool vec = (reinterpret_cast<uintptr_t>(a.out) | (a.ld * sizeof(T))) % 16 == 0;
     const uint32_t chunks = (uint32_t)((a.cols + 511) / 512);
-    const uint64_t blocks = (a.rows * chunks + 3) / 4;
-    k_mx_dequantize<T><<<dim3((uint32_t)blocks), 256, 0, s>>>(a, chunks, vec);
+    const uint64_t most = most_blocks(256) * 4 / chunks;   // rows of a launch
+    for (uint64_t r = 0; r < a.rows; r += most) {
+        MxDequantizeArgs part = a;
+        part.codes += r * mx_code_bytes(a.cols);
+        part.scales += r * mx_scale_bytes(a.cols);
+        part.rows = a.rows - r < most ? a.rows - r : most;
+        part.out = static_cast<T *>(a.out) + r * a.ld;
+        k_mx_dequantize<T><<<dim3((uint32_t)((part.rows * chunks + 3) / 4)), 256, 0, s>>>(part, chunks, vec);
+    }
     return hipGetLastError();
 }
 

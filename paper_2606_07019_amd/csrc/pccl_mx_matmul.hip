@@ -452,6 +452,7 @@ inline uint32_t stages_each(uint64_t m, uint64_t n, uint64_t k)
     return (uint32_t)(per < stages ? per : stages + (stages == 0));
 }
 inline uint64_t padded(uint64_t n) { return (n + 3) / 4 * 4; }
+inline uint64_t big_tiles(uint64_t m, uint64_t n) { return ((m + 255) / 256) * ((n + 255) / 256); }
 
 // 256 x 256 sums a workgroup where such tiles occupy every compute unit: four
 // products for two operands read from LDS.  128 x 128 otherwise, eight waves all
@@ -460,8 +461,7 @@ template <class T>
 hipError_t tiles_of(const MxMatmulArgs &a, bool vec, hipStream_t s)
 {
     const uint32_t stages = (uint32_t)(mx_steps(a.k) + 1) / 2;
-    const uint64_t big = ((a.m + 255) / 256) * ((a.n + 255) / 256);
-    if (big >= 256) return tiled<T, 256, 256, 4, 2>(a, stages + 1, s);
+    if (big_tiles(a.m, a.n) >= 256) return tiled<T, 256, 256, 4, 2>(a, stages + 1, s);
     const uint32_t per = stages_each(a.m, a.n, a.k);
     if (per >= stages) return tiled<T, 128, 128, 4, 4>(a, per, s);
     MxMatmulArgs part = a;
@@ -482,6 +482,9 @@ size_t mx_matmul_workspace(uint64_t m, uint64_t n, uint64_t k)
     if (few_rows(m, k) || per >= stages) return 0;
     return (size_t)((stages + per - 1) / per * m * padded(n) * sizeof(float));
 }
+
+// Few rows take 512 workgroups at most, smaller tiles 1,024 and less.
+bool mx_matmul_fits(uint64_t m, uint64_t n, uint64_t k) { return few_rows(m, k) || big_tiles(m, n) <= most_blocks(512); }
 
 hipError_t launch_mx_matmul(const MxMatmulArgs &a, uint32_t dtype, hipStream_t s)
 {

@@ -37,6 +37,10 @@ inline __host__ __device__ uint64_t mx_scale_bytes(uint64_t cols) { return mx_st
 // extent fit 32 bits; products of two are computed in 64 bits.
 constexpr uint64_t OPS_MAX_EXTENT = 0x7FFFFFFFull;
 
+// A launch has fewer than 2^32 threads.  Kernels whose rows do not meet take
+// more of them in further launches.
+inline constexpr uint64_t most_blocks(uint32_t threads) { return 0xFFFFFFFFull / threads; }
+
 // The product's k: a tile's 256 rows of codes stay within 32-bit offsets.
 constexpr uint64_t MX_MAX_K = 1ull << 24;
 
@@ -72,6 +76,7 @@ struct MxMatmulArgs {
     float *part;                     // partial sums of a split k, or null
 };
 size_t mx_matmul_workspace(uint64_t m, uint64_t n, uint64_t k);
+bool mx_matmul_fits(uint64_t m, uint64_t n, uint64_t k);   // one launch's threads
 hipError_t launch_mx_matmul(const MxMatmulArgs &a, uint32_t dtype, hipStream_t s);
 
 struct RouteArgs {

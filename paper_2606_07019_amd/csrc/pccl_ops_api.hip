@@ -108,7 +108,7 @@ pccl_status check_packed(pccl_ctx *c, const char *name, const void *codes, const
 // A launch of `blocks` workgroups must stay below 2^32 threads.
 pccl_status check_grid(pccl_ctx *c, uint64_t blocks, uint32_t threads)
 {
-    LIMIT(blocks <= 0xFFFFFFFFull / threads, "%llu workgroups in one launch (limit %llu)", (ull)blocks, (ull)(0xFFFFFFFFull / threads));
+    LIMIT(blocks <= most_blocks(threads), "%llu workgroups in one launch (limit %llu)", (ull)blocks, (ull)most_blocks(threads));
     return PCCL_OK;
 }
 
@@ -167,7 +167,7 @@ pccl_status pccl_mx_quantize(pccl_ctx *c, const void *x, pccl_dtype dtype, uint6
         NEED(codes || scales || codes_t || scales_t, "no output");
         if (codes || scales) TRY(check_packed(c, "rows", codes, scales));
         if (codes_t || scales_t) TRY(check_packed(c, "columns", codes_t, scales_t));
-        TRY(check_grid(c, ((rows + 127) / 128) * ((cols + 127) / 128), 256));
+        if (codes_t) TRY(check_grid(c, ((rows + 127) / 128) * ((cols + 127) / 128), 256));
         OnDevice device;
         TRY(device.enter(c));
         const MxQuantizeArgs a{x, rows, cols, ld, codes, scales, codes_t, scales_t};
@@ -183,7 +183,6 @@ pccl_status pccl_mx_dequantize(pccl_ctx *c, const uint8_t *codes, const uint8_t 
         TRY(check_rows(c, "out", out, rows, cols, ld, elem_bytes(dtype)));
         if (rows == 0 || cols == 0) return PCCL_OK;
         TRY(check_packed(c, "input", codes, scales));
-        TRY(check_grid(c, (rows * ((cols + 511) / 512) + 3) / 4, 256));
         OnDevice device;
         TRY(device.enter(c));
         const MxDequantizeArgs a{codes, scales, rows, cols, ld, out};
@@ -215,7 +214,7 @@ pccl_status pccl_mx_matmul(pccl_ctx *c, const uint8_t *a_codes, const uint8_t *a
             TRY(check_packed(c, "a", a_codes, a_scales));
             TRY(check_packed(c, "b", b_codes, b_scales));
         }
-        TRY(check_grid(c, ((m + 127) / 128) * ((n + 15) / 16), 512));
+        LIMIT(mx_matmul_fits(m, n, k), "%llu x %llu (limit 2^23 - 1 tiles of 256 x 256)", (ull)m, (ull)n);
         TRY(check_space(c, workspace, workspace_bytes, mx_matmul_workspace(m, n, k)));
         OnDevice device;
         TRY(device.enter(c));
@@ -272,7 +271,6 @@ pccl_status pccl_moe_route_backward(pccl_ctx *c, const void *logits, pccl_dtype 
         NEED(weights && aligned(weights, 4), "weights are null or misaligned");
         NEED(ids && aligned(ids, 4), "ids are null or misaligned");
         NEED(dweights && aligned(dweights, 4), "dweights are null or misaligned");
-        TRY(check_grid(c, (tokens + 3) / 4, 256));
         OnDevice device;
         TRY(device.enter(c));
         const RouteBackwardArgs a{logits, tokens, ld, ld_d, experts, topk, normalize ? 1u : 0u, token_mask, weights, ids, dweights, dlogits};

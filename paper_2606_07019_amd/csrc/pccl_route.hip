@@ -331,7 +331,18 @@ struct Backward {
     {
         const bool vec = whole<T, V>(a.dlogits, a.ld_d) && (a.normalize || whole<T, V>(a.logits, a.ld));
         constexpr uint32_t per = BACK_WAVES * 64 / LANES;
-        k_route_backward<T, LANES, V><<<dim3((uint32_t)((a.tokens + per - 1) / per)), BACK_THREADS, 0, s>>>(a, vec);
+        constexpr uint64_t most = most_blocks(BACK_THREADS) * per;   // rows of a launch
+        for (uint64_t r = 0; r < a.tokens; r += most) {
+            RouteBackwardArgs part = a;
+            part.tokens = a.tokens - r < most ? a.tokens - r : most;
+            if (a.logits) part.logits = static_cast<const T *>(a.logits) + r * a.ld;
+            if (a.mask) part.mask += r;
+            part.weights += r * a.topk;
+            part.ids += r * a.topk;
+            part.dweights += r * a.topk;
+            part.dlogits = static_cast<T *>(a.dlogits) + r * a.ld_d;
+            k_route_backward<T, LANES, V><<<dim3((uint32_t)((part.tokens + per - 1) / per)), BACK_THREADS, 0, s>>>(part, vec);
+        }
         return hipGetLastError();
     }
 };
