@@ -4,7 +4,8 @@ Argument marshalling over the C ABI (include/pccl.h, "operators at the ends of
 a collective"): shapes and types are checked here, the rest by the library,
 and every step runs in its HIP kernels.  Calls are queued on the current
 stream of the device; outputs and workspaces come from torch's allocator, so
-calls on different streams do not share any.
+calls on different streams do not share any.  Threads may share an Operators:
+their calls take turns.
 
     ops = Operators()
     q = ops.quantize(x)                          # rows in 4.25 bits a value
@@ -15,6 +16,7 @@ calls on different streams do not share any.
 
 from __future__ import annotations
 
+import threading
 from typing import NamedTuple, Optional
 
 import torch
@@ -50,6 +52,7 @@ class Operators:
         self.device = torch.device("cuda", device)
         self._index = device
         self.h = None
+        self._lock = threading.Lock()   # a context takes one call at a time, its message included
         self._lib = P.load_library()
         self._spaces = {}
         with torch.cuda.device(self.device):   # both calls make it the current one and leave it so
@@ -99,9 +102,11 @@ class Operators:
     def _empty(self, dtype, *shape):
         return torch.empty(*shape, dtype=dtype, device=self.device)
 
-    def _call(self, status):
-        if status:
-            P._check(self.h, status)
+    def _call(self, function, *args):
+        with self._lock:
+            status = function(self.h, *args)
+            if status:
+                P._check(self.h, status)
 
     def _space(self, ask, *sizes):
         """(workspace, its address, its size) of the call that `ask` gives the size for."""
@@ -109,7 +114,8 @@ class Operators:
         if nbytes is None:
             if len(self._spaces) >= 4096:   # a caller whose sizes keep changing
                 self._spaces.clear()
-            nbytes = self._spaces[ask, sizes] = ask(self.h, *sizes)
+            with self._lock:
+                nbytes = self._spaces[ask, sizes] = ask(self.h, *sizes)
         if not nbytes:
             return None, None, 0
         ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
@@ -128,8 +134,7 @@ class Operators:
             cb, sb = mx_bytes(rows)
             c = MX(self._empty(torch.uint8, cols, cb), self._empty(torch.uint8, cols, sb), rows)
             cc, cs = c.codes.data_ptr(), c.scales.data_ptr()
-        self._call(self._lib.pccl_mx_quantize(self.h, x.data_ptr(), _DTYPE[x.dtype], rows, cols, ld, rc, rs, cc, cs,
-                                              self._stream()))
+        self._call(self._lib.pccl_mx_quantize, x.data_ptr(), _DTYPE[x.dtype], rows, cols, ld, rc, rs, cc, cs, self._stream())
         return r, c
 
     def quantize(self, x) -> MX:
@@ -150,8 +155,7 @@ class Operators:
         rows = q.codes.shape[0]
         codes, scales = self._packed("q", q, (rows,))
         out = self._empty(dtype, rows, q.cols)
-        self._call(self._lib.pccl_mx_dequantize(self.h, codes, scales, rows, q.cols, out.data_ptr(), kind,
-                                                q.cols, self._stream()))
+        self._call(self._lib.pccl_mx_dequantize, codes, scales, rows, q.cols, out.data_ptr(), kind, q.cols, self._stream())
         return out
 
     def matmul(self, a: MX, b: MX, dtype, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -169,8 +173,7 @@ class Operators:
             if (rows, cols) != (m, n) or out.dtype != dtype:
                 raise ValueError(f"out: {(m, n)} of {dtype} is needed, got {(rows, cols)} of {out.dtype}")
         ws, wp, nbytes = self._space(P.pccl_mx_matmul_workspace, m, n, k)
-        self._call(self._lib.pccl_mx_matmul(self.h, ac, as_, bc, bs, m, n, k, out.data_ptr(), kind, ld, wp,
-                                            nbytes, self._stream()))
+        self._call(self._lib.pccl_mx_matmul, ac, as_, bc, bs, m, n, k, out.data_ptr(), kind, ld, wp, nbytes, self._stream())
         return out
 
     # -- router ----------------------------------------------------------------
@@ -184,9 +187,8 @@ class Operators:
         ids = self._empty(torch.int32, tokens, topk)
         counts = self._empty(torch.int32, experts)
         order = self._empty(torch.int32, tokens * topk)
-        self._call(self._lib.pccl_moe_route(self.h, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld,
-                                            topk, normalize, mp, weights.data_ptr(), ids.data_ptr(),
-                                            counts.data_ptr(), order.data_ptr(), wp, nbytes, self._stream()))
+        self._call(self._lib.pccl_moe_route, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld, topk, normalize, mp,
+                   weights.data_ptr(), ids.data_ptr(), counts.data_ptr(), order.data_ptr(), wp, nbytes, self._stream())
         return weights, ids, counts, order
 
     def route_backward(self, logits, weights, ids, dweights, normalize: bool = True,
@@ -196,11 +198,11 @@ class Operators:
         topk = weights.shape[1] if weights.dim() == 2 else 0
         shape = (tokens, topk)
         out = self._empty(logits.dtype, tokens, experts)
-        self._call(self._lib.pccl_moe_route_backward(
-            self.h, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld, topk, normalize,
+        self._call(
+            self._lib.pccl_moe_route_backward, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld, topk, normalize,
             None if mask is None else self._mask(mask, tokens), self._same("weights", weights, shape, torch.float32),
             self._same("ids", ids, shape, torch.int32), self._same("dweights", dweights, shape, torch.float32),
-            out.data_ptr(), experts, self._stream()))
+            out.data_ptr(), experts, self._stream())
         return out
 
     # -- mixture-of-experts layer ------------------------------------------------
@@ -228,17 +230,18 @@ class Operators:
             dp, ds = self._same("down", down, (experts, hidden, inter), dtype), None
         ws, wp, nbytes = self._space(P.pccl_moe_layer_workspace, tokens, experts, topk, hidden, inter)
         y = self._empty(dtype, tokens, hidden)
-        self._call(self._lib.pccl_moe_layer(
-            self.h, x.data_ptr(), _DTYPE[dtype], ld, tokens, experts, topk, hidden, inter, normalize,
+        self._call(
+            self._lib.pccl_moe_layer, x.data_ptr(), _DTYPE[dtype], ld, tokens, experts, topk, hidden, inter, normalize,
             None if mask is None else self._mask(mask, tokens), rp, upp, ups, dp, ds, y.data_ptr(), hidden, wp, nbytes,
-            self._stream()))
+            self._stream())
         return y
 
     def close(self):
-        if self.h is not None:
+        with self._lock:
             h, self.h = self.h, None
-            with torch.cuda.device(self.device):
-                P.pccl_destroy(h)
+            if h is not None:
+                with torch.cuda.device(self.device):
+                    P.pccl_destroy(h)
 
     def __del__(self):
         try:
