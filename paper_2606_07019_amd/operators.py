@@ -7,6 +7,11 @@ stream of the device; outputs and workspaces come from torch's allocator, so
 calls on different streams do not share any.  Threads may share an Operators:
 their calls take turns.
 
+Of torch's automatic differentiation, route()'s weights carry the router's
+gradient.  Packed values are whole numbers and have none: a training step makes
+its three products itself, of operands packed along the axis that each sums
+over.  moe_layer() is for serving; asked for a gradient, its result raises.
+
     ops = Operators()
     q = ops.quantize(x)                          # rows in 4.25 bits a value
     y = ops.matmul(q, w, torch.bfloat16)         # q w^T
@@ -20,6 +25,8 @@ import threading
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
+from torch.autograd.function import once_differentiable
 
 from paper_2606_07019_amd import pccl as P
 
@@ -38,6 +45,46 @@ def mx_bytes(cols: int):
     """(code bytes, scale bytes) of one packed row of `cols` values."""
     steps = -(-cols // 128)
     return steps * 64, steps * 4
+
+
+def _learns(*tensors):
+    """Whether a derivative is recorded for one of the tensors; RuntimeError for a forward-mode one, which none has here."""
+    if forward_ad._current_level >= 0 and any(forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise RuntimeError("the operators have no forward-mode derivatives")
+    return torch.is_grad_enabled() and any(t.requires_grad for t in tensors)
+
+
+class _Route(torch.autograd.Function):
+    """route() with its gradient."""
+
+    @staticmethod
+    def forward(ctx, logits, ops, topk, normalize, mask):
+        weights, ids, counts, order = ops._route(logits, topk, normalize, mask)
+        ctx.mark_non_differentiable(ids, counts, order)
+        # normalised weights' gradient does not read the logits
+        ctx.save_for_backward(None if normalize else logits, weights, ids, mask)
+        ctx.rest = ops, logits.shape, logits.dtype, normalize
+        return weights, ids, counts, order
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dweights, *_):
+        ops, shape, dtype, normalize = ctx.rest
+        logits, weights, ids, mask = ctx.saved_tensors
+        return ops._route_backward(logits, shape, dtype, weights, ids, dweights.contiguous(), normalize, mask), None, None, None, None
+
+
+class _Served(torch.autograd.Function):
+    """A result without a gradient, for inputs that a gradient is asked of."""
+
+    @staticmethod
+    def forward(ctx, name, call, *inputs):
+        ctx.name = name
+        return call(*inputs)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"{ctx.name} has no gradient")
 
 
 class Operators:
@@ -172,6 +219,10 @@ class Operators:
             rows, cols, ld = self._matrix("out", out)
             if (rows, cols) != (m, n) or out.dtype != dtype:
                 raise ValueError(f"out: {(m, n)} of {dtype} is needed, got {(rows, cols)} of {out.dtype}")
+            if _learns(out):
+                raise ValueError("out: a tensor that requires grad is not written")
+            if not out.is_inference():
+                torch.autograd.graph.increment_version(out)
         ws, wp, nbytes = self._space(P.pccl_mx_matmul_workspace, m, n, k)
         self._call(self._lib.pccl_mx_matmul, ac, as_, bc, bs, m, n, k, out.data_ptr(), kind, ld, wp, nbytes, self._stream())
         return out
@@ -179,7 +230,12 @@ class Operators:
     # -- router ----------------------------------------------------------------
 
     def route(self, logits, topk: int, normalize: bool = True, mask: Optional[torch.Tensor] = None):
-        """(weights, ids, counts, order) of the topk largest logits of every row."""
+        """(weights, ids, counts, order) of the topk largest logits of every row; the weights carry the gradient."""
+        if _learns(logits):
+            return _Route.apply(logits, self, topk, normalize, mask)
+        return self._route(logits, topk, normalize, mask)
+
+    def _route(self, logits, topk, normalize, mask):
         tokens, experts, ld = self._matrix("logits", logits)
         mp = None if mask is None else self._mask(mask, tokens)
         ws, wp, nbytes = self._space(P.pccl_moe_route_workspace, tokens, experts, topk)
@@ -194,12 +250,19 @@ class Operators:
     def route_backward(self, logits, weights, ids, dweights, normalize: bool = True,
                        mask: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The gradient of route()'s weights with respect to its logits, in their type."""
-        tokens, experts, ld = self._matrix("logits", logits)
+        return self._route_backward(logits, logits.shape, logits.dtype, weights, ids, dweights, normalize, mask)
+
+    def _route_backward(self, logits, shape, dtype, weights, ids, dweights, normalize, mask):
+        if logits is None:
+            (tokens, experts), ld, address = shape, shape[1], None
+        else:
+            tokens, experts, ld = self._matrix("logits", logits)
+            address = logits.data_ptr()
         topk = weights.shape[1] if weights.dim() == 2 else 0
         shape = (tokens, topk)
-        out = self._empty(logits.dtype, tokens, experts)
+        out = self._empty(dtype, tokens, experts)
         self._call(
-            self._lib.pccl_moe_route_backward, logits.data_ptr(), _DTYPE[logits.dtype], tokens, experts, ld, topk, normalize,
+            self._lib.pccl_moe_route_backward, address, _DTYPE[dtype], tokens, experts, ld, topk, normalize,
             None if mask is None else self._mask(mask, tokens), self._same("weights", weights, shape, torch.float32),
             self._same("ids", ids, shape, torch.int32), self._same("dweights", dweights, shape, torch.float32),
             out.data_ptr(), experts, self._stream())
@@ -212,6 +275,13 @@ class Operators:
         """y [tokens, hidden] for x [tokens, hidden], router [experts, hidden],
         up [experts, 2 inter, hidden] (gate rows first) and down [experts,
         hidden, inter], the latter two of x's type or packed (MX)."""
+        tensors = (x, router) if isinstance(up, MX) or isinstance(down, MX) else (x, router, up, down)
+        if _learns(*tensors):
+            return _Served.apply("moe_layer", lambda x, router, up, down: self._moe_layer(x, router, up, down, topk, normalize, mask),
+                                 x, router, up, down)
+        return self._moe_layer(x, router, up, down, topk, normalize, mask)
+
+    def _moe_layer(self, x, router, up, down, topk, normalize, mask):
         dtype = x.dtype
         tokens, hidden, ld = self._matrix("x", x, (torch.bfloat16, torch.float16))
         experts = router.shape[0]
