@@ -401,8 +401,12 @@ template <int MT, int S>
 hipError_t skinny_as(const MxMatmulArgs &a, uint32_t dtype, bool vec, hipStream_t s)
 {
     const uint32_t tiles = (uint32_t)((a.n + 15) / 16);
-    // one workgroup a compute unit, or two where their registers leave room
-    constexpr uint32_t most = MT * S <= 8 ? 512u : 256u;
+    // Two workgroups a compute unit where a wave holds one or two steps, one
+    // beyond (B from memory, with 256 and with 512 workgroups: 1 x 65536 x 1024
+    // 19.9 and 13.0 us, 64 x 65536 x 2048 27.4 and 22.7, 64 x 16384 x 2048 9.5 and
+    // 10.5, 1 x 16384 x 5120 12.3 and 13.9, 64 x 16384 x 4096 13.1 and 16.5; three
+    // and four steps of one row over the longest n alone gain with 512, 33.0 and 30.0)
+    constexpr uint32_t most = S <= 2 ? 512u : 256u;
     constexpr int ahead = MT * S <= 16 ? 2 : 1;
     k_mx_skinny<MT, S, ahead><<<dim3(tiles < most ? tiles : most), 64 * SKINNY_WAVES, 0, s>>>(a, dtype, vec, tiles);
     return hipGetLastError();
@@ -434,7 +438,11 @@ hipError_t tiled(const MxMatmulArgs &a, uint32_t per, hipStream_t s)
     return hipGetLastError();
 }
 
-// Few rows, and k short enough for eight waves to hold their operands.
+// Few rows, and k short enough for eight waves to hold their operands.  Against
+// the form for many rows, B from memory: 1 x 4096 x 4096 5.0 and 11.3 us, 64 x
+// 4096 x 4096 7.1 and 13.4, 64 x 1024 x 8192 9.3 and 12.7, 64 x 65536 x 2048 23.5
+// and 25.8; nothing is left at 64 rows with the shortest k (64 x 16384 x 1024 8.1
+// and 7.6).
 inline bool few_rows(uint64_t m, uint64_t k) { return m <= 64 && mx_steps(k) <= SKINNY_WAVES * SKINNY_MAX_STEPS; }
 
 // Stages of k that a workgroup of 128 x 128 sums takes: all, or, where such
@@ -443,9 +451,10 @@ inline bool few_rows(uint64_t m, uint64_t k) { return m <= 64 && mx_steps(k) <= 
 // 22 us in eight parts, 256 x 1024 x 8192 28 and 15; with parts of 16 stages the
 // latter takes 19, and 1000 x 1000 x 4096, where two parts gain least, 16 either way.
 constexpr uint32_t LEAST_STAGES = 8;
+inline uint64_t small_tiles(uint64_t m, uint64_t n) { return ((m + 127) / 128) * ((n + 127) / 128); }
 inline uint32_t stages_each(uint64_t m, uint64_t n, uint64_t k)
 {
-    const uint64_t stages = (mx_steps(k) + 1) / 2, tiles = ((m + 127) / 128) * ((n + 127) / 128), want = tiles < 256 ? 256 / tiles : 1;
+    const uint64_t stages = (mx_steps(k) + 1) / 2, tiles = small_tiles(m, n), want = tiles < 256 ? 256 / tiles : 1;
     uint64_t per = (stages + want - 1) / want;
     if (per < LEAST_STAGES) per = LEAST_STAGES;
     per = (per + 3) / 4 * 4;
@@ -454,14 +463,18 @@ inline uint32_t stages_each(uint64_t m, uint64_t n, uint64_t k)
 inline uint64_t padded(uint64_t n) { return (n + 3) / 4 * 4; }
 inline uint64_t big_tiles(uint64_t m, uint64_t n) { return ((m + 255) / 256) * ((n + 255) / 256); }
 
-// 256 x 256 sums a workgroup where such tiles occupy every compute unit: four
-// products for two operands read from LDS.  128 x 128 otherwise, eight waves all
-// the same: two to a SIMD (2040 x 1500 x 8192 29.1 us, with four waves 30.7).
+// 256 x 256 sums a workgroup, four products for two operands read from LDS, where
+// such tiles occupy half of the compute units and smaller ones would not be done
+// in one round (256 and 128 either way, k of 8192: 64 tiles of 256, 2048 x 2048,
+// 58 and 32 us; 81, 2300 x 2300, 61 and 56; 128, 2048 x 4096, 60 and 61; 144, 3000 x
+// 3000, 61 and 87; 1024, 8192 x 8192, 303 and 458; but 128 x 32768, 256 of the
+// smaller ones, 62 and 42).  128 x 128 otherwise, eight waves all the same: two to a
+// SIMD (2040 x 1500 x 8192 29.1 us, with four waves 30.7).
 template <class T>
 hipError_t tiles_of(const MxMatmulArgs &a, bool vec, hipStream_t s)
 {
     const uint32_t stages = (uint32_t)(mx_steps(a.k) + 1) / 2;
-    if (big_tiles(a.m, a.n) >= 256) return tiled<T, 256, 256, 4, 2>(a, stages + 1, s);
+    if (big_tiles(a.m, a.n) >= 128 && small_tiles(a.m, a.n) > 256) return tiled<T, 256, 256, 4, 2>(a, stages + 1, s);
     const uint32_t per = stages_each(a.m, a.n, a.k);
     if (per >= stages) return tiled<T, 128, 128, 4, 4>(a, per, s);
     MxMatmulArgs part = a;
@@ -483,7 +496,7 @@ size_t mx_matmul_workspace(uint64_t m, uint64_t n, uint64_t k)
     return (size_t)((stages + per - 1) / per * m * padded(n) * sizeof(float));
 }
 
-// Few rows take 512 workgroups at most, smaller tiles 1,024 and less.
+// Few rows take 512 workgroups at most, smaller tiles a few hundred.
 bool mx_matmul_fits(uint64_t m, uint64_t n, uint64_t k) { return few_rows(m, k) || big_tiles(m, n) <= most_blocks(512); }
 
 hipError_t launch_mx_matmul(const MxMatmulArgs &a, uint32_t dtype, hipStream_t s)
