@@ -809,13 +809,15 @@ __global__ __launch_bounds__(256) void k_moe_sum(MoeArgs a, MoeSpace m)
     static_cast<T *>(a.y)[(uint64_t)t * a.ld_y + h] = Elem<T>::put(v);
 }
 
-// Whether each wave has tiles of its own rather than a quarter of the blocks of
-// a workgroup's: where a quarter is less than four blocks, so that rounding up
-// leaves waves without work, and the tiles of the experts in use (at most
-// `most`) are enough to keep every compute unit's waves busy all the same.
-// 1536 inner values in 4 bits are six blocks: 80 us shared, 66 us this way;
-// 4096 in 4 bits are 16: 98 us shared, 110 us this way.
-inline bool own_tiles(uint64_t blocks, uint64_t tiles, uint64_t most) { return blocks < 4 * WAVES && tiles * most >= 2048; }
+// Whether each wave has tiles of its own rather than a part of the blocks of a
+// workgroup's: where sharing leaves less than two blocks a wave, so that
+// rounding up leaves waves without work, and the tiles of the experts in use (at
+// most `most`) are enough to keep every compute unit's waves busy all the same.
+// Whole layers, shared and this way, 16 tokens, 8 of 128 experts in 4 bits: 1024
+// x 256 values (one block) 37 and 32 us, 1024 x 512 47 and 44, 4096 x 1536 (six)
+// 226 and 216, 1024 x 2048 (eight) 100 and 103, 1024 x 3840 171 and 179; fewer
+// tiles, 1024 x 1024: 2048 of them 59 and 58, 1024 38 and 39, 512 25 and 28.
+inline bool own_tiles(uint64_t blocks, uint64_t tiles, uint64_t most) { return blocks < 2 * WAVES && tiles * most >= 2048; }
 
 template <class T, class W, bool VEC, int NT>
 hipError_t experts_as(const MoeArgs &a, const MoeSpace &m, hipStream_t s)
@@ -837,12 +839,17 @@ hipError_t experts_as(const MoeArgs &a, const MoeSpace &m, hipStream_t s)
 }
 
 // Tiles of 16 tokens that share one reading of the weights: one where experts
-// have eight tokens on average at most (few have more than 16, and theirs are
-// read again), four otherwise, at the price of registers.
+// have a few tokens on average (few have more than 16, and theirs are read
+// again, from the caches), four beyond, at the price of registers.  Weights in 4
+// bits cost less to read again and more registers to unpack.  64 experts of 2048
+// x 1400, 8 picks, one and four: in 16 bits 64 tokens 249 and 254 us, 96 269 and
+// 268, 128 320 and 292, 256 497 and 357; in 4 bits 128 tokens 186 and 188, 192 222
+// and 216, 256 288 and 256.
 template <class T, class W, bool VEC>
 hipError_t experts_of(const MoeArgs &a, const MoeSpace &m, hipStream_t s)
 {
-    if (a.tokens <= 16 || (uint64_t)a.tokens * a.topk <= 8ull * a.experts) return experts_as<T, W, VEC, 1>(a, m, s);
+    const uint64_t few = a.up_scales ? 24 : 12;   // tokens of an expert
+    if (a.tokens <= 16 || (uint64_t)a.tokens * a.topk <= few * a.experts) return experts_as<T, W, VEC, 1>(a, m, s);
     return experts_as<T, W, VEC, 4>(a, m, s);
 }
 
