@@ -51,7 +51,10 @@ def _learns(*tensors):
     """Whether a derivative is recorded for one of the tensors; RuntimeError for a forward-mode one, which none has here."""
     if forward_ad._current_level >= 0 and any(forward_ad.unpack_dual(t).tangent is not None for t in tensors):
         raise RuntimeError("the operators have no forward-mode derivatives")
-    return torch.is_grad_enabled() and any(t.requires_grad for t in tensors)
+    for t in tensors:
+        if t.requires_grad:
+            return torch.is_grad_enabled()
+    return False
 
 
 class _Route(torch.autograd.Function):
@@ -102,8 +105,13 @@ class Operators:
         self._lock = threading.Lock()   # a context takes one call at a time, its message included
         self._lib = P.load_library()
         self._spaces = {}
-        with torch.cuda.device(self.device):   # both calls make it the current one and leave it so
-            self.h = P.pccl_create(device, 0)
+        try:
+            with torch.cuda.device(self.device):   # making and closing a context leave it the current one
+                self.h = P.pccl_create(device, 0)
+        except P.PcclError:
+            raise
+        except RuntimeError as e:
+            raise P.PcclError(5, f"cannot create a context on HIP device {device}") from e
 
     # -- checks ------------------------------------------------------------
 

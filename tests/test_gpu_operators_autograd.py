@@ -140,3 +140,17 @@ def test_inference_tensors_are_taken(ops):   # noqa: F811
         np.testing.assert_allclose(_np(out), _np(want) @ _np(want).T, atol=64 * 2.0 ** -20)
         w, ids, _, _ = ops.route(out, 2)
         assert ids.shape == (8, 2)
+
+
+def test_layer_of_packed_weights_has_no_gradient_and_says_so(ops):   # noqa: F811
+    print("[operators] layer of packed weights asked for a gradient", flush=True)
+    from paper_2606_07019_amd.operators import MX
+    t = _torch()
+    x, router = t.randn(3, 64, device="cuda").bfloat16(), t.randn(4, 64, device="cuda").bfloat16()
+    up, down = (MX(*(f.view(4, w.shape[1], -1) for f in ops.quantize(w.view(-1, w.shape[2]))[:2]), w.shape[2])
+                for w in (t.randn(4, 64, 64, device="cuda"), t.randn(4, 64, 32, device="cuda")))
+    want = ops.moe_layer(x, router, up, down, 2)
+    y = ops.moe_layer(x.clone().requires_grad_(), router, up, down, 2)
+    assert t.equal(y, want) and not want.requires_grad
+    with pytest.raises(RuntimeError, match="no gradient"):
+        y.float().sum().backward()

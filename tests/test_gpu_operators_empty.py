@@ -41,3 +41,11 @@ def test_example_with_fewer_tokens_than_experts():
     spec.loader.exec_module(example)
     r = example.run(tokens=3)
     assert r["counts"].sum() == 4 * 3 * 2 and np.isfinite(r["off"])
+
+
+def test_a_device_that_is_not_there():
+    from paper_2606_07019_amd import pccl as P
+    from paper_2606_07019_amd.operators import Operators
+    with pytest.raises(P.PcclError) as e:
+        Operators(64)
+    assert e.value.name == "PCCL_EDEVICE"
