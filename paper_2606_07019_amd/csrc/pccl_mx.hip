@@ -153,14 +153,12 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantizeArgs a, uint32_t 
             for (int i = 0; i < Oct<T>::W; i++) o[p].w[i] = 0;
         }
     }
-    {
 #pragma unroll
-        for (int p = 0; p < 8; p++) {
-            u32x4 *q = reinterpret_cast<u32x4 *>(&part[wave][((p * 4 + (lane >> 4)) * TILE + c0) * sizeof(T) / 4]);
+    for (int p = 0; p < 8; p++) {
+        u32x4 *q = reinterpret_cast<u32x4 *>(&part[wave][((p * 4 + (lane >> 4)) * TILE + c0) * sizeof(T) / 4]);
 #pragma unroll
-            for (int i = 0; i < Oct<T>::W / 4; i++)
-                q[i] = u32x4{o[p].w[4 * i], o[p].w[4 * i + 1], o[p].w[4 * i + 2], o[p].w[4 * i + 3]};
-        }
+        for (int i = 0; i < Oct<T>::W / 4; i++)
+            q[i] = u32x4{o[p].w[4 * i], o[p].w[4 * i + 1], o[p].w[4 * i + 2], o[p].w[4 * i + 3]};
     }
     if (ROWS) {
 #pragma unroll
@@ -179,84 +177,82 @@ __global__ __launch_bounds__(256) void k_mx_quantize(MxQuantizeArgs a, uint32_t 
             }
         }
     }
-    {
-        __syncthreads();
-        const uint64_t cbt = mx_code_bytes(a.rows), sbt = mx_scale_bytes(a.rows);
-        const uint32_t c = lane * 2;
-        u32x4 out[2];
-        uint32_t byte[2];
-        if constexpr (sizeof(T) == 4) {
-            float v[2][32];
-            uint32_t top[2] = {0, 0};
+    __syncthreads();
+    const uint64_t cbt = mx_code_bytes(a.rows), sbt = mx_scale_bytes(a.rows);
+    const uint32_t c = lane * 2;
+    u32x4 out[2];
+    uint32_t byte[2];
+    if constexpr (sizeof(T) == 4) {
+        float v[2][32];
+        uint32_t top[2] = {0, 0};
 #pragma unroll
-            for (int r = 0; r < 32; r++) {
-                const u32x2 w = *reinterpret_cast<const u32x2 *>(&part[wave][r * TILE + c]);
-                v[0][r] = __uint_as_float(w.x);
-                v[1][r] = __uint_as_float(w.y);
-                const uint32_t p = w.x & 0x7FFFFFFFu, q = w.y & 0x7FFFFFFFu;
-                top[0] = p > top[0] ? p : top[0];
-                top[1] = q > top[1] ? q : top[1];
-            }
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                byte[h] = MxIn<T>::byte(top[h]);
-                const float s = mx_scale(byte[h]);
-#pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    uint32_t t = 0;
-                    t = cvt2<0>(t, v[h][8 * q], v[h][8 * q + 1], s);
-                    t = cvt2<1>(t, v[h][8 * q + 2], v[h][8 * q + 3], s);
-                    t = cvt2<2>(t, v[h][8 * q + 4], v[h][8 * q + 5], s);
-                    t = cvt2<3>(t, v[h][8 * q + 6], v[h][8 * q + 7], s);
-                    out[h][q] = byte[h] == 255u ? 0u : t;
-                }
-            }
-        } else {
-            uint32_t w[32];
-            u16x2 top = {0, 0};
-#pragma unroll
-            for (int r = 0; r < 32; r++) {
-                w[r] = part[wave][r * (TILE / 2) + lane];
-                top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[r] & 0x7FFF7FFFu));
-            }
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                byte[h] = MxIn<T>::byte(h ? top.y : top.x);
-                const float s = mx_scale(byte[h]);
-                const uint32_t sel = h ? 0x07060302u : 0x05040100u;   // the column's halves of two rows
-#pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    uint32_t t = 0;
-                    t = cvt2<T, 0>(t, __builtin_amdgcn_perm(w[8 * q + 1], w[8 * q], sel), s);
-                    t = cvt2<T, 1>(t, __builtin_amdgcn_perm(w[8 * q + 3], w[8 * q + 2], sel), s);
-                    t = cvt2<T, 2>(t, __builtin_amdgcn_perm(w[8 * q + 5], w[8 * q + 4], sel), s);
-                    t = cvt2<T, 3>(t, __builtin_amdgcn_perm(w[8 * q + 7], w[8 * q + 6], sel), s);
-                    out[h][q] = byte[h] == 255u ? 0u : t;
-                }
-            }
+        for (int r = 0; r < 32; r++) {
+            const u32x2 w = *reinterpret_cast<const u32x2 *>(&part[wave][r * TILE + c]);
+            v[0][r] = __uint_as_float(w.x);
+            v[1][r] = __uint_as_float(w.y);
+            const uint32_t p = w.x & 0x7FFFFFFFu, q = w.y & 0x7FFFFFFFu;
+            top[0] = p > top[0] ? p : top[0];
+            top[1] = q > top[1] ? q : top[1];
         }
-        // the columns' codes go out by way of LDS, 64 bytes of a column at a
-        // time; piece w of column c stands at (w + c / 2) % 4 of the column
-        __syncthreads();
-        u32x4 *out_lds = reinterpret_cast<u32x4 *>(part);
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            tsc[c + h][wave] = (uint8_t)byte[h];
-            out_lds[(c + h) * 4u + ((wave + lane) & 3u)] = out[h];
-        }
-        __syncthreads();
+            byte[h] = MxIn<T>::byte(top[h]);
+            const float s = mx_scale(byte[h]);
 #pragma unroll
-        for (uint32_t i = 0; i < 2; i++) {
-            const uint32_t at = i * 64u + threadIdx.x / 4, w = threadIdx.x % 4;
-            const uint64_t cc = (uint64_t)tc * TILE + at;
-            if (cc < a.cols)
-                *reinterpret_cast<u32x4 *>(a.codes_t + cc * cbt + (uint64_t)tr * (TILE / 2) + w * 16u) = out_lds[at * 4u + ((w + at / 2) & 3u)];
+            for (int q = 0; q < 4; q++) {
+                uint32_t t = 0;
+                t = cvt2<0>(t, v[h][8 * q], v[h][8 * q + 1], s);
+                t = cvt2<1>(t, v[h][8 * q + 2], v[h][8 * q + 3], s);
+                t = cvt2<2>(t, v[h][8 * q + 4], v[h][8 * q + 5], s);
+                t = cvt2<3>(t, v[h][8 * q + 6], v[h][8 * q + 7], s);
+                out[h][q] = byte[h] == 255u ? 0u : t;
+            }
         }
-        const uint64_t cc = (uint64_t)tc * TILE + threadIdx.x;
-        if (threadIdx.x < TILE && cc < a.cols)
-            *reinterpret_cast<uint32_t *>(a.scales_t + cc * sbt + (uint64_t)tr * 4u) =
-                *reinterpret_cast<const uint32_t *>(tsc[threadIdx.x]);
+    } else {
+        uint32_t w[32];
+        u16x2 top = {0, 0};
+#pragma unroll
+        for (int r = 0; r < 32; r++) {
+            w[r] = part[wave][r * (TILE / 2) + lane];
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[r] & 0x7FFF7FFFu));
+        }
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            byte[h] = MxIn<T>::byte(h ? top.y : top.x);
+            const float s = mx_scale(byte[h]);
+            const uint32_t sel = h ? 0x07060302u : 0x05040100u;   // the column's halves of two rows
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                uint32_t t = 0;
+                t = cvt2<T, 0>(t, __builtin_amdgcn_perm(w[8 * q + 1], w[8 * q], sel), s);
+                t = cvt2<T, 1>(t, __builtin_amdgcn_perm(w[8 * q + 3], w[8 * q + 2], sel), s);
+                t = cvt2<T, 2>(t, __builtin_amdgcn_perm(w[8 * q + 5], w[8 * q + 4], sel), s);
+                t = cvt2<T, 3>(t, __builtin_amdgcn_perm(w[8 * q + 7], w[8 * q + 6], sel), s);
+                out[h][q] = byte[h] == 255u ? 0u : t;
+            }
+        }
     }
+    // the columns' codes go out by way of LDS, 64 bytes of a column at a
+    // time; piece w of column c stands at (w + c / 2) % 4 of the column
+    __syncthreads();
+    u32x4 *out_lds = reinterpret_cast<u32x4 *>(part);
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        tsc[c + h][wave] = (uint8_t)byte[h];
+        out_lds[(c + h) * 4u + ((wave + lane) & 3u)] = out[h];
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < 2; i++) {
+        const uint32_t at = i * 64u + threadIdx.x / 4, w = threadIdx.x % 4;
+        const uint64_t cc = (uint64_t)tc * TILE + at;
+        if (cc < a.cols)
+            *reinterpret_cast<u32x4 *>(a.codes_t + cc * cbt + (uint64_t)tr * (TILE / 2) + w * 16u) = out_lds[at * 4u + ((w + at / 2) & 3u)];
+    }
+    const uint64_t cc = (uint64_t)tc * TILE + threadIdx.x;
+    if (threadIdx.x < TILE && cc < a.cols)
+        *reinterpret_cast<uint32_t *>(a.scales_t + cc * sbt + (uint64_t)tr * 4u) =
+            *reinterpret_cast<const uint32_t *>(tsc[threadIdx.x]);
 }
 
 // The rows alone: a wave packs 512 values of eight rows at a time, so that what
