@@ -476,7 +476,7 @@ pccl_status pccl_moe_route_workspace(pccl_ctx *ctx, uint64_t tokens, uint32_t ex
  *     weights, over the whole row or, with `normalize`, over the picks.  A
  *     logit of minus infinity bars its expert; where fewer than topk are left
  *     the other picks are -1 with weight 0.  A NaN counts as the largest and
- *     makes its row's weights NaN.
+ *     makes its row's weights NaN, as an infinity does.
  *   token_mask: one byte a token, 0 = padding (no picks), or NULL.
  *   counts[experts]: the picks of each expert.
  *   order[tokens * topk]: the slots (token * topk + position) by expert, those

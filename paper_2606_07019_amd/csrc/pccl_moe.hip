@@ -547,8 +547,8 @@ __device__ inline f32x4 up_products(const u32x4 (&p)[N], const u32x4 (&b)[N], f3
 }
 
 // Gate and up rows: sub-tiles 2 i and 2 i + 1 of a wave's tile.  Bound by reading
-// them: 64 tokens, 64 experts of 2048 x 1400 in 16 bits 134 us (5.5 TB/s), 16
-// tokens, 128 experts of 4096 x 1536 in 4 bits 94 us (4.9 TB/s).
+// them: 64 tokens, 64 experts of 2048 x 1400 in 16 bits 136 us (5.4 TB/s), 16
+// tokens, 128 experts of 4096 x 1536 in 4 bits 95 us (4.8 TB/s).
 template <class T, class W, bool VEC, int M, int NT, bool SHARE>
 __global__ __launch_bounds__(64 * WAVES) void k_moe_up(MoeArgs a, MoeSpace m, uint32_t len, uint32_t slen)
 {

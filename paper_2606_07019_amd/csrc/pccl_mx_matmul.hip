@@ -7,7 +7,7 @@
 // second.  B goes first, so a lane's sums are neighbours in out.
 //
 // The form with 32 rows of each operand over 64 values of k is the faster one
-// (6.8 PFLOP/s from registers with random values, 4.3 for 16 rows) and serves
+// (6.6 PFLOP/s from registers with random values, 4.6 for 16 rows) and serves
 // many rows: lane l gives row l % 32, one block, and gets sixteen sums, four
 // neighbours in rows 8 q + 4 (l / 32) of the first operand.
 #include "pccl_ops.h"
@@ -78,7 +78,8 @@ constexpr uint32_t SKINNY_MAX_STEPS = 8;   // steps of k a wave holds A's operan
 // read in the operands' order every lane's 16 bytes cost a cycle of the compute
 // unit's port, and 48 x 16384 x 5120 took 38 us), AHEAD tiles ahead, turns it
 // round through LDS, and the waves' sums are joined there in their order.  48 x
-// 16384 x 5120 takes 14 us (B at 3.2 TB/s), 1 x 4096 x 4096 4.6.
+// 16384 x 5120 takes 15 us with B from memory (3.0 TB/s), 14 from the device's
+// cache; 1 x 4096 x 4096 5.0 and 4.6.
 template <int MT, int S, int AHEAD>
 __global__ __launch_bounds__(64 * SKINNY_WAVES) void k_mx_skinny(MxMatmulArgs a, uint32_t dtype, bool vec, uint32_t tiles)
 {
@@ -197,8 +198,10 @@ struct Index {
 // registers the next one is read from LDS, and a stage's last step is
 // multiplied after the next one's first is on its way.  In LDS chunk c (16
 // bytes) of row r stands at chunk c ^ (r / 2 % 8) of the row, so the 16 lanes
-// that read one chunk of 16 rows meet every bank once.  8192^3 takes 310 us by
-// itself (3.5 PFLOP/s).
+// that read one chunk of 16 rows meet every bank once.  8192^3 takes 306 us by
+// itself (3.6 PFLOP/s): the matrix units are busy 45 % of its cycles, LDS reads 23
+// %, and waves wait 30 % of their time, since every stage's barrier brings the two
+// waves of a SIMD to the same point.
 // Two chunks of scales go with two stages of codes (LDS holds no more), three
 // with up to four.
 constexpr int scale_chunks(int buffers) { return buffers == 2 ? 2 : 3; }

@@ -42,3 +42,18 @@ def test_types_that_are_not_taken(ops):
             ops.dequantize(q, bad)
         with pytest.raises(ValueError):
             ops.matmul(q, q, bad)
+
+
+@pytest.mark.parametrize("normalize", [True, False])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+def test_an_infinite_logit_leaves_no_weights(ops, dtype, normalize):
+    # infinity less infinity: the row's softmax is no number, its picks are what they are, and no other row knows
+    import torch
+    print(f"[operators] infinite logit {dtype} {normalize}", flush=True)
+    l = torch.zeros((3, 70), dtype=getattr(torch, dtype), device="cuda")
+    l[1, 66], l[1, 4], l[2, 5] = float("inf"), 3.0, 1.0
+    w, ids, counts, _ = ops.route(l, 2, normalize=normalize)
+    assert ids.tolist() == [[0, 1], [66, 4], [5, 0]]
+    assert torch.isnan(w[1]).all() and torch.isfinite(w[[0, 2]]).all()
+    d = ops.route_backward(l, w, ids, torch.ones_like(w), normalize=normalize)
+    assert torch.isnan(d[1, [66, 4]]).all() and torch.isfinite(d[[0, 2]]).all()
