@@ -1,6 +1,8 @@
 // Internal definitions of the operators at the ends of a collective: packing
 // to microscaled 4-bit values, their product, the router and the
-// mixture-of-experts layer (not part of the ABI).
+// mixture-of-experts layer; packing to 8 bits with a scale for 128 values, the
+// products and experts' products of that, and the router's balance loss (not
+// part of the ABI).
 #pragma once
 
 #include <atomic>
@@ -121,6 +123,99 @@ struct MoeArgs {
 };
 size_t moe_workspace(uint32_t tokens, uint32_t experts, uint32_t topk, uint32_t hidden, uint32_t inter);
 hipError_t launch_moe(const MoeArgs &a, uint32_t dtype, hipStream_t s);
+
+// Rows of 8-bit floating point: blocks of 128 values share a scale.  A stored
+// row ends on a whole block, padded with zeros, and its scales on a whole word.
+constexpr uint32_t F8_BLOCK = 128;
+inline __host__ __device__ uint64_t f8_blocks(uint64_t cols) { return (cols + F8_BLOCK - 1) / F8_BLOCK; }
+inline __host__ __device__ uint64_t f8_code_bytes(uint64_t cols) { return f8_blocks(cols) * F8_BLOCK; }
+inline __host__ __device__ uint64_t f8_scale_bytes(uint64_t cols) { return (f8_blocks(cols) + 3) / 4 * 4; }
+
+// The product's k: a tile's 256 rows of codes stay within 32-bit offsets.
+constexpr uint64_t F8_MAX_K = 1ull << 23;
+
+// Rows in expert order, cut into blocks of up to 128 rows of one expert (and of
+// up to 256, for larger tiles).  The table, in words: experts + 1 numbers of
+// blocks before each expert, then two words a block (its first row; its expert
+// and rows, expert | rows << 16), no rows in those that are not used; then the
+// larger blocks the same way.
+inline __host__ __device__ uint64_t groups_blocks(uint64_t experts, uint64_t rows, uint32_t block)
+{
+    return rows / block + (experts < rows ? experts : rows);
+}
+struct GroupsArgs {
+    const int32_t *counts;
+    uint64_t rows;
+    uint32_t experts, pad;
+    uint64_t blocks, blocks2;    // of 128 rows, of 256
+    int32_t *table;
+};
+inline __host__ __device__ uint64_t groups_words(uint64_t experts, uint64_t rows)
+{
+    return experts + 1 + 2 * groups_blocks(experts, rows, 128) + 2 * groups_blocks(experts, rows, 256);
+}
+hipError_t launch_groups(const GroupsArgs &a, hipStream_t s);
+
+struct F8QuantizeArgs {
+    const void *x;
+    uint64_t batch, rows, cols, ld;   // `batch` matrices, one behind the other
+    uint8_t *codes, *scales;          // of the rows, or null
+    uint8_t *codes_t, *scales_t;      // of the columns, or null
+    uint32_t tiles;                   // a scale for 128 x 128 values, the same for rows and columns
+    uint32_t experts;                 // of the blocks of rows
+    const int32_t *groups;            // the columns' blocks are those of this table; or null
+};
+hipError_t launch_f8_quantize(const F8QuantizeArgs &a, uint32_t dtype, hipStream_t s);
+
+struct F8DequantizeArgs {
+    const uint8_t *codes, *scales;
+    uint64_t rows, cols, ld;
+    void *out;
+};
+hipError_t launch_f8_dequantize(const F8DequantizeArgs &a, uint32_t dtype, hipStream_t s);
+
+struct F8MatmulArgs {
+    const uint8_t *a, *as, *b, *bs;  // codes and scales of the m rows and of the n rows
+    uint64_t m, n, k, ld;
+    void *out;
+    float *part;                     // partial sums of a split k, or null
+    const int32_t *groups;           // experts' products: the table
+    uint64_t rows;                   // of all experts
+    uint32_t experts;
+};
+size_t f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k);
+bool f8_matmul_fits(uint64_t m, uint64_t n, uint64_t k);   // one launch's threads
+hipError_t launch_f8_matmul(const F8MatmulArgs &a, uint32_t dtype, hipStream_t s);
+// out [rows][n]: rows of a times their expert's b [n][k]
+bool f8_experts_fit(uint64_t rows, uint32_t experts, uint64_t n);
+hipError_t launch_f8_expert_matmul(const F8MatmulArgs &a, uint32_t dtype, hipStream_t s);
+// out [experts][m][n]: m rows of a times n rows of b over each expert's blocks
+bool f8_gradients_fit(uint32_t experts, uint64_t m, uint64_t n);
+hipError_t launch_f8_expert_gradient(const F8MatmulArgs &a, uint32_t dtype, hipStream_t s);
+
+struct BalanceArgs {
+    const void *logits;
+    uint64_t tokens, ld;
+    uint32_t experts, topk;
+    const uint8_t *mask;
+    const int32_t *ids;
+    float *loss, *probs;
+    int32_t *counts, *rows;
+    char *ws;
+};
+size_t balance_workspace(uint64_t tokens, uint32_t experts);
+hipError_t launch_balance(const BalanceArgs &a, uint32_t dtype, hipStream_t s);
+
+struct BalanceBackwardArgs {
+    const void *logits;
+    uint64_t tokens, ld, ld_d;
+    uint32_t experts, pad;
+    const uint8_t *mask;
+    const int32_t *counts, *rows;
+    const float *dloss, *dprobs;   // either may be null
+    void *dlogits;
+};
+hipError_t launch_balance_backward(const BalanceBackwardArgs &a, uint32_t dtype, hipStream_t s);
 
 #ifdef __HIPCC__
 // Lets a kernel have `bytes` of LDS on the current device, once for each device.

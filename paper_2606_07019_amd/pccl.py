@@ -83,6 +83,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "pccl_moe_layer_workspace": ([P, U32, U32, U32, U32, U32, ctypes.POINTER(ctypes.c_size_t)], I),
         "pccl_moe_layer": ([P, P, I, U64, U32, U32, U32, U32, U32, I, P, P, P, P, P, P, P, U64, P,
                             ctypes.c_size_t, P], I),
+        "pccl_moe_groups": ([P, P, U32, U64, P, P], I),
+        "pccl_f8_quantize": ([P, P, I, U64, U64, U64, U64, I, P, P, P, P, P], I),
+        "pccl_f8_quantize_experts": ([P, P, I, U64, U64, U64, P, U32, P, P, P, P, P], I),
+        "pccl_f8_dequantize": ([P, P, P, U64, U64, P, I, U64, P], I),
+        "pccl_f8_matmul_workspace": ([P, U64, U64, U64, ctypes.POINTER(ctypes.c_size_t)], I),
+        "pccl_f8_matmul": ([P, P, P, P, P, U64, U64, U64, P, I, U64, P, ctypes.c_size_t, P], I),
+        "pccl_f8_expert_matmul": ([P, P, P, P, P, U64, U32, U64, U64, P, P, I, U64, P], I),
+        "pccl_f8_expert_gradient": ([P, P, P, P, P, U64, U32, U64, U64, P, P, I, P], I),
+        "pccl_moe_balance_workspace": ([P, U64, U32, ctypes.POINTER(ctypes.c_size_t)], I),
+        "pccl_moe_balance": ([P, P, I, U64, U32, U64, P, U32, P, P, P, P, P, P, ctypes.c_size_t, P], I),
+        "pccl_moe_balance_backward": ([P, P, I, U64, U32, U64, P, P, P, P, P, P, U64, P], I),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -326,6 +337,68 @@ def pccl_moe_layer(h, x, dtype, ld_x, tokens, experts, topk, hidden, inter, norm
     _check(h, load_library().pccl_moe_layer(h, x, dtype, ld_x, tokens, experts, topk, hidden, inter, normalize,
                                             token_mask, router, up, up_scales, down, down_scales, y, ld_y,
                                             workspace, nbytes, stream_ptr or None))
+
+
+def pccl_moe_groups(h, counts, experts, rows, groups, stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_moe_groups(h, counts, experts, rows, groups, stream_ptr or None))
+
+
+def pccl_f8_quantize(h, x, dtype, batch, rows, cols, ld, tiles=0, codes=None, scales=None, codes_t=None, scales_t=None,
+                     stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_f8_quantize(h, x, dtype, batch, rows, cols, ld, tiles, codes, scales, codes_t,
+                                              scales_t, stream_ptr or None))
+
+
+def pccl_f8_quantize_experts(h, x, dtype, rows, cols, ld, groups, experts, codes=None, scales=None, codes_t=None,
+                             scales_t=None, stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_f8_quantize_experts(h, x, dtype, rows, cols, ld, groups, experts, codes, scales,
+                                                      codes_t, scales_t, stream_ptr or None))
+
+
+def pccl_f8_dequantize(h, codes, scales, rows, cols, out, dtype, ld, stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_f8_dequantize(h, codes, scales, rows, cols, out, dtype, ld, stream_ptr or None))
+
+
+def pccl_f8_matmul_workspace(h, m, n, k) -> int:
+    out = ctypes.c_size_t()
+    _check(h, load_library().pccl_f8_matmul_workspace(h, m, n, k, ctypes.byref(out)))
+    return int(out.value)
+
+
+def pccl_f8_matmul(h, a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld, workspace=None, nbytes=0,
+                   stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_f8_matmul(h, a_codes, a_scales, b_codes, b_scales, m, n, k, out, dtype, ld,
+                                            workspace, nbytes, stream_ptr or None))
+
+
+def pccl_f8_expert_matmul(h, a_codes, a_scales, b_codes, b_scales, rows, experts, n, k, groups, out, dtype, ld,
+                          stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_f8_expert_matmul(h, a_codes, a_scales, b_codes, b_scales, rows, experts, n, k,
+                                                   groups, out, dtype, ld, stream_ptr or None))
+
+
+def pccl_f8_expert_gradient(h, a_codes, a_scales, b_codes, b_scales, rows, experts, m, n, groups, out, dtype,
+                            stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_f8_expert_gradient(h, a_codes, a_scales, b_codes, b_scales, rows, experts, m, n,
+                                                     groups, out, dtype, stream_ptr or None))
+
+
+def pccl_moe_balance_workspace(h, tokens, experts) -> int:
+    out = ctypes.c_size_t()
+    _check(h, load_library().pccl_moe_balance_workspace(h, tokens, experts, ctypes.byref(out)))
+    return int(out.value)
+
+
+def pccl_moe_balance(h, logits, dtype, tokens, experts, ld, ids, topk, token_mask, loss, probs, counts, rows,
+                     workspace=None, nbytes=0, stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_moe_balance(h, logits, dtype, tokens, experts, ld, ids, topk, token_mask, loss,
+                                              probs, counts, rows, workspace, nbytes, stream_ptr or None))
+
+
+def pccl_moe_balance_backward(h, logits, dtype, tokens, experts, ld, token_mask, counts, rows, dloss, dprobs,
+                              dlogits, ld_d, stream_ptr: int = 0) -> None:
+    _check(h, load_library().pccl_moe_balance_backward(h, logits, dtype, tokens, experts, ld, token_mask, counts,
+                                                       rows, dloss, dprobs, dlogits, ld_d, stream_ptr or None))
 
 
 # ---- convenience wrapper (marshalling of a whole workload) --------------------
