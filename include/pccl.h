@@ -550,7 +550,7 @@ pccl_status pccl_moe_layer(pccl_ctx *ctx, const void *x, pccl_dtype dtype, uint6
 #define PCCL_GROUP_BLOCKS(experts, rows) \
     ((uint64_t)(rows) / 128 + ((uint64_t)(experts) < (uint64_t)(rows) ? (uint64_t)(experts) : (uint64_t)(rows)))
 #define PCCL_GROUP_WORDS(experts, rows)                                                                \
-    ((uint64_t)(experts) + 1 + 2 * PCCL_GROUP_BLOCKS(experts, rows) + 2 * ((uint64_t)(rows) / 256) +   \
+    ((uint64_t)(experts) + 2 + 2 * PCCL_GROUP_BLOCKS(experts, rows) + 2 * ((uint64_t)(rows) / 256) +   \
      2 * ((uint64_t)(experts) < (uint64_t)(rows) ? (uint64_t)(experts) : (uint64_t)(rows)))
 pccl_status pccl_moe_groups(pccl_ctx *ctx, const int32_t *counts, uint32_t experts, uint64_t rows,
                             int32_t *groups, void *hip_stream);

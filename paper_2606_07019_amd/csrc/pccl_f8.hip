@@ -59,12 +59,12 @@ __global__ __launch_bounds__(GROUP_THREADS) void k_groups(GroupsArgs a)
     }
     __syncthreads();
     if (blockIdx.x == 0)
-        for (uint32_t i = e; i <= a.experts; i += GROUP_THREADS) a.table[i] = (int32_t)start[0][i];
+        for (uint32_t i = e; i <= a.experts + 1; i += GROUP_THREADS) a.table[i] = (int32_t)(i <= a.experts ? start[0][i] : start[1][a.experts]);
     const uint64_t all = a.blocks + a.blocks2;
     for (uint64_t j = (uint64_t)blockIdx.x * GROUP_THREADS + e; j < all; j += (uint64_t)gridDim.x * GROUP_THREADS) {
         const uint32_t l = j >= a.blocks, size = 128u << l;
         const uint32_t b = (uint32_t)(l ? j - a.blocks : j);
-        int32_t *out = a.table + a.experts + 1 + 2 * j;
+        int32_t *out = a.table + a.experts + 2 + 2 * j;
         if (b >= start[l][a.experts]) {
             out[0] = out[1] = 0;
             continue;
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_
     uint64_t first = (uint64_t)matrix * a.rows + (uint64_t)tr * TILE;
     uint32_t n = (uint32_t)(a.rows - (uint64_t)tr * TILE < TILE ? a.rows - (uint64_t)tr * TILE : TILE);
     if (a.groups) {
-        const int32_t *entry = a.groups + a.experts + 1 + 2 * (uint64_t)tr;
+        const int32_t *entry = a.groups + a.experts + 2 + 2 * (uint64_t)tr;
         first = (uint32_t)entry[0];
         n = (uint32_t)entry[1] >> 16;
         if (n == 0) return;

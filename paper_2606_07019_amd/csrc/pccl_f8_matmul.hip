@@ -39,16 +39,17 @@ __device__ inline bf16x8 wide(uint32_t w0, uint32_t w1, float scale)
     return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 
-// c[i][j] += y[j] x[i] over 64 values of k.
-template <bool EXACT, int TM, int TN>
+// c[i][j] += y[j] x[i] over 64 values of k, for products FROM up to TO in the
+// order of c; a scale is the lowest byte of its word.
+template <bool EXACT, int FROM, int TO, int TM, int TN>
 __device__ inline void products(f32x16 (&c)[TM][TN], const Piece (&x)[TM], const uint32_t (&xs)[TM], const Piece (&y)[TN], const uint32_t (&ys)[TN])
 {
     if constexpr (EXACT) {
         float fx[TM], fy[TN];
 #pragma unroll
-        for (int i = 0; i < TM; i++) fx[i] = mx_scale(xs[i]);
+        for (int i = 0; i < TM; i++) fx[i] = mx_scale(xs[i] & 0xFFu);
 #pragma unroll
-        for (int j = 0; j < TN; j++) fy[j] = mx_scale(ys[j]);
+        for (int j = 0; j < TN; j++) fy[j] = mx_scale(ys[j] & 0xFFu);
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             bf16x8 wx[TM], wy[TN];
@@ -63,17 +64,31 @@ __device__ inline void products(f32x16 (&c)[TM][TN], const Piece (&x)[TM], const
                 wx[i] = wide(v[q % 2 * 2], v[q % 2 * 2 + 1], fx[i]);
             }
 #pragma unroll
-            for (int i = 0; i < TM; i++)
-#pragma unroll
-                for (int j = 0; j < TN; j++) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wy[j], wx[i], c[i][j], 0, 0, 0);
+            for (int p = FROM; p < TO; p++) c[p / TN][p % TN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wy[p % TN], wx[p / TN], c[p / TN][p % TN], 0, 0, 0);
         }
     } else {
         auto whole = [](const Piece &p) { return i32x8{(int)p.lo.x, (int)p.lo.y, (int)p.lo.z, (int)p.lo.w, (int)p.hi.x, (int)p.hi.y, (int)p.hi.z, (int)p.hi.w}; };
 #pragma unroll
-        for (int i = 0; i < TM; i++)
+        for (int p = FROM; p < TO; p++) {
+            const int i = p / TN, j = p % TN;
+            c[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(y[j]), whole(x[i]), c[i][j], 0, 0, 0, (int)ys[j], 0, (int)xs[i]);
+        }
+    }
+    // keeps them in front of what follows: nothing else would
 #pragma unroll
-            for (int j = 0; j < TN; j++)
-                c[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(y[j]), whole(x[i]), c[i][j], 0, 0, 0, (int)ys[j], 0, (int)xs[i]);
+    for (int p = FROM; p < TO; p++) asm volatile("" : "+a"(c[p / TN][p % TN]));
+}
+
+// The order of N products with READS reads from LDS and COPIES copies evenly between them.
+template <int N, int READS, int COPIES, int I = 0>
+__device__ inline void mixed()
+{
+    if constexpr (I < N) {
+        constexpr int r = (I + 1) * READS / N - I * READS / N, c = (I + 1) * COPIES / N - I * COPIES / N;
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+        if constexpr (c > 0) __builtin_amdgcn_sched_group_barrier(0x020, c, 0);
+        mixed<N, READS, COPIES, I + 1>();
     }
 }
 
@@ -94,12 +109,17 @@ __device__ inline void store4(T *out, uint64_t ld, uint64_t row, uint64_t col, u
         if (col + i < n) p[i] = t[i];
 }
 
+template <int N>
+struct Number {
+    static constexpr int value = N;
+};
+
 // What a workgroup multiplies.
 enum Kind { DENSE, EXPERTS, GRADIENT };
 struct Job {
     const uint8_t *a, *as, *b, *bs;   // the tile's first rows
     uint32_t rows_a, rows_b;          // of them there are, at most the tile's
-    uint32_t first, stages;           // blocks of k
+    uint32_t first, blocks;           // of k
     uint64_t row, col;                // of out (GRADIENT: in the expert's part)
     uint32_t slice;                   // of the partial sums, or the expert
 };
@@ -118,20 +138,26 @@ __device__ inline void deal(uint32_t id, uint32_t mt, uint32_t nt, uint32_t &m, 
     n = in / gm;
 }
 
-// A tile of BM x BN sums, WM x WN waves.  A stage is a block of 128 values of k
-// (128 bytes a row), copied from memory straight to LDS, BUFFERS stages in a
-// ring; scales come for four stages at a time, a word a row.  A stage has two
-// instruction steps.  While one step is multiplied from registers the next is
-// read from LDS; the barrier stands between a stage's two steps, when all its
-// operands have been read and the next stage's have landed, so that no step
-// waits for its reads.  In LDS chunk c (16 bytes) of row r stands at chunk c ^
-// (r / 2 % 8) of the row, so the 16 lanes that read one chunk of 16 rows meet
-// every bank once.
+// A tile of BM x BN sums, WM x WN waves.  A stage is a block of 128 values of k,
+// copied from memory straight to LDS in whole pieces of 128 bytes a row (with
+// pieces of 64 bytes a compute unit copies 63 GB/s, with these 115), BUFFERS
+// stages in a ring; scales come for four stages at a time, a word a row.
+// A stage's two instruction steps are three parts:
+//   1  step 0's first products; step 1 is read from LDS
+//      everyone has read the stage
+//   2  the rest of step 0's and as many of step 1's; copies of a later stage to its place
+//      the next stage has landed for everyone
+//   3  the rest of step 1's; step 0 of the next stage is read, the other copies
+// so that copies go out evenly (16 in a row hold up the wave's products) and have
+// a whole stage's time.  In LDS chunk c (16 bytes) of row r stands at chunk c ^ (r
+// / 2 % 8) of the row, so the 16 lanes that read one chunk of 16 rows meet every
+// bank once.
 template <class T, bool EXACT, Kind KIND, int BM, int BN, int WM, int WN, int BUFFERS>
 __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uint32_t mt, uint32_t nt, uint32_t per)
 {
     constexpr uint32_t THREADS = 64 * WM * WN, PASS = THREADS / 8;   // rows of codes that the workgroup copies at a time
-    constexpr int TM = BM / WM / 32, TN = BN / WN / 32, PA = BM / PASS, PB = BN / PASS, COPIES = PA + PB;
+    constexpr int TM = BM / WM / 32, TN = BN / WN / 32, PA = BM / PASS, PB = BN / PASS;
+    constexpr uint32_t SCALES = (BM + BN + THREADS - 1) / THREADS, COPIES = PA + PB;   // a stage's, scales left out
     constexpr uint32_t STAGE = (BM + BN) * 128, CODES = BUFFERS * STAGE, WORDS = (BM + BN) * 4;   // a stage's codes, all; four stages' scales
     constexpr uint32_t ALL = CODES + 4 * WORDS;
     static_assert(BM % PASS == 0 && BN % PASS == 0 && BM % 64 == 0 && BN % 64 == 0, "whole passes");
@@ -143,6 +169,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
     Job job;
     {
         uint32_t ti, tj;
+        if constexpr (KIND == EXPERTS) {   // the blocks that there are, not those that there could be
+            mt = (uint32_t)__builtin_amdgcn_readfirstlane(a.groups[a.experts + (BM == 256)]);
+            if (blockIdx.x >= mt * nt) return;
+        }
         deal(blockIdx.x, mt, nt, ti, tj);
         const uint64_t m0 = (uint64_t)ti * BM, n0 = (uint64_t)tj * BN;
         job.col = n0;
@@ -151,11 +181,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
         job.bs = a.bs + n0 * sb;
         if constexpr (KIND == EXPERTS) {
             const uint64_t skip = BM == 256 ? groups_blocks(a.experts, a.rows, 128) : 0;
-            const int32_t *entry = a.groups + a.experts + 1 + 2 * (skip + ti);
+            const int32_t *entry = a.groups + a.experts + 2 + 2 * (skip + ti);
             const uint32_t word = (uint32_t)__builtin_amdgcn_readfirstlane(entry[1]), expert = word & 0xFFFFu;
             job.row = (uint32_t)__builtin_amdgcn_readfirstlane(entry[0]);
             job.rows_a = word >> 16;
-            if (job.rows_a == 0) return;
             job.b += expert * a.n * cb;
             job.bs += expert * a.n * sb;
         } else {
@@ -168,11 +197,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
         if constexpr (KIND == GRADIENT) {
             const int32_t *start = a.groups + blockIdx.y;
             job.first = (uint32_t)__builtin_amdgcn_readfirstlane(start[0]);
-            job.stages = (uint32_t)__builtin_amdgcn_readfirstlane(start[1]) - job.first;
+            job.blocks = (uint32_t)__builtin_amdgcn_readfirstlane(start[1]) - job.first;
         } else {
             const uint32_t all = (uint32_t)f8_blocks(a.k);
             job.first = KIND == DENSE ? blockIdx.y * per : 0u;
-            job.stages = KIND == DENSE && all - job.first > per ? per : all - job.first;
+            job.blocks = KIND == DENSE && all - job.first > per ? per : all - job.first;
         }
     }
     // what this thread copies of a stage: a chunk of every PASS-th row of A,
@@ -189,26 +218,27 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
         const uint32_t row = i * PASS + tid / 8;
         offb[i] = (row < ln ? row : ln) * cb + chunk;
     }
-    const uint32_t stages = job.stages, last = stages - 1u;
-    auto copy = [&](uint32_t stage) {   // past the last stage: that one again, into a buffer nobody reads
-        uint8_t *to = lds + stage % BUFFERS * STAGE;
+    const uint32_t stages = job.blocks, last = stages - 1u;
+    auto copy = [&](uint32_t stage, int i) {   // past the last stage: that one again, into a buffer nobody reads
         const uint32_t k = (job.first + (stage < last ? stage : last)) * 128u;
-#pragma unroll
-        for (int i = 0; i < PA; i++)
-            __builtin_amdgcn_global_load_lds((gptr)(job.a + (offa[i] + k)), (lptr)(to + (i * THREADS + wave * 64u) * 16u), 16, 0, 0);
-#pragma unroll
-        for (int i = 0; i < PB; i++)
-            __builtin_amdgcn_global_load_lds((gptr)(job.b + (offb[i] + k)), (lptr)(to + BM * 128u + (i * THREADS + wave * 64u) * 16u), 16, 0, 0);
+        uint8_t *to = lds + stage % BUFFERS * STAGE + (i * THREADS + wave * 64u) * 16u;
+        if (i < PA) __builtin_amdgcn_global_load_lds((gptr)(job.a + (offa[i] + k)), (lptr)to, 16, 0, 0);
+        else __builtin_amdgcn_global_load_lds((gptr)(job.b + (offb[i - PA] + k)), (lptr)to, 16, 0, 0);
     };
-    // the scales of blocks 4 w ... + 3 of every row
-    auto copy_scales = [&](uint32_t w) {
-        const uint32_t at = (w * 4u < sb ? w * 4u : sb - 4u);
+    // the scales of blocks 4 w ... + 3, a word of every row; a wave's rows are one operand's
+    uint32_t offs[SCALES];
 #pragma unroll
-        for (uint32_t i = 0; i < (BM + BN + THREADS - 1) / THREADS; i++) {
-            const uint32_t row = i * THREADS + tid;
-            if (row - lane >= BM + BN) break;   // whole waves
-            const uint8_t *from = row < BM ? job.as + ((row < lm ? row : lm) * sb + at) : job.bs + ((row - BM < ln ? row - BM : ln) * sb + at);
-            __builtin_amdgcn_global_load_lds((gptr)from, (lptr)(lds + CODES + w % 4u * WORDS + (i * THREADS + wave * 64u) * 4u), 4, 0, 0);
+    for (uint32_t i = 0; i < SCALES; i++) {
+        const uint32_t first = i * THREADS + wave * 64u, row = (first < BM ? first : first - BM) + lane, lim = first < BM ? lm : ln;
+        offs[i] = (row < lim ? row : lim) * sb;
+    }
+    auto copy_scales = [&](uint32_t w) {
+        const uint32_t at = w * 4u < sb ? w * 4u : sb - 4u;
+#pragma unroll
+        for (uint32_t i = 0; i < SCALES; i++) {
+            const uint32_t first = i * THREADS + wave * 64u;
+            if (first >= BM + BN) break;
+            __builtin_amdgcn_global_load_lds((gptr)((first < BM ? job.as : job.bs) + (offs[i] + at)), (lptr)(lds + CODES + w % 4u * WORDS + first * 4u), 4, 0, 0);
         }
     };
 
@@ -220,57 +250,89 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
         uint32_t x[TM], y[TN];
     };
     const uint32_t key = r / 2 % 8;
-    auto read = [&](Held &h, uint32_t stage, uint32_t step) {
-        const uint8_t *from = lds + stage % BUFFERS * STAGE + r * 128u;
+    auto read = [&](Held &h, uint32_t stage, uint32_t step, int q) {
         const uint32_t c = step * 4u + half * 2u, lo = (c ^ key) * 16u, hi = ((c + 1u) ^ key) * 16u;
-#pragma unroll
-        for (int j = 0; j < TN; j++) {
-            const uint8_t *p = from + (BM + wn + j * 32u) * 128u;
-            h.y[j] = Piece{*reinterpret_cast<const u32x4 *>(p + lo), *reinterpret_cast<const u32x4 *>(p + hi)};
-        }
-#pragma unroll
-        for (int i = 0; i < TM; i++) {
-            const uint8_t *p = from + (wm + i * 32u) * 128u;
-            h.x[i] = Piece{*reinterpret_cast<const u32x4 *>(p + lo), *reinterpret_cast<const u32x4 *>(p + hi)};
-        }
+        const uint8_t *p = lds + stage % BUFFERS * STAGE + (r + (q < TN ? BM + wn + q * 32u : wm + (q - TN) * 32u)) * 128u;
+        const Piece got{*reinterpret_cast<const u32x4 *>(p + lo), *reinterpret_cast<const u32x4 *>(p + hi)};
+        if (q < TN) h.y[q] = got;
+        else h.x[q - TN] = got;
     };
     auto read_scales = [&](Scales &to, uint32_t stage) {
-        const uint32_t block = job.first + stage, shift = block % 4u * 8u;
-        const uint8_t *from = lds + CODES + block / 4u % 4u * WORDS + r * 4u;
-        auto byte = [&](uint32_t row) { return *reinterpret_cast<const uint32_t *>(from + row * 4u) >> shift & 0xFFu; };
+        const uint8_t *from = lds + CODES + (job.first + stage) / 4u % 4u * WORDS + r * 4u;
+        auto word = [&](uint32_t row) { return *reinterpret_cast<const uint32_t *>(from + row * 4u); };
 #pragma unroll
-        for (int j = 0; j < TN; j++) to.y[j] = byte(BM + wn + j * 32u);
+        for (int j = 0; j < TN; j++) to.y[j] = word(BM + wn + j * 32u);
 #pragma unroll
-        for (int i = 0; i < TM; i++) to.x[i] = byte(wm + i * 32u);
+        for (int i = 0; i < TM; i++) to.x[i] = word(wm + i * 32u);
     };
-    // the next stage has landed for everyone (the COPIES of later ones may be under way), and nobody reads this one any more
-    auto ready = [&]() {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFFERS - 2) * COPIES) : "memory");
+    auto bytes_of = [&](const Scales &words, uint32_t stage) {   // at the words' ends
+        const uint32_t shift = (job.first + stage) % 4u * 8u;
+        Scales to;
+#pragma unroll
+        for (int j = 0; j < TN; j++) to.y[j] = words.y[j] >> shift;
+#pragma unroll
+        for (int i = 0; i < TM; i++) to.x[i] = words.x[i] >> shift;
+        return to;
+    };
+    auto meet = [&]() {
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
     };
+    auto all_read = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        meet();
+    };
+    auto landed = [&](auto later) {   // but for so many later copies
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(later)::value) : "memory");
+        meet();
+    };
+    // without it the compiler turns the reads before the loop and at its end into ones at its beginning, for which products wait
+    auto held_back = []() { asm volatile("" ::: "memory"); };
+    constexpr int N = TM * TN, READS = 2 * (TM + TN), PART = EXACT ? N / 4 : N * 3 / 8, CUT = EXACT ? COPIES / 2 : COPIES * 3 / 4;   // products of a step, its reads; what the second part takes
     f32x16 acc[TM][TN] = {};
     if (stages) {
         copy_scales(job.first / 4u);
         copy_scales(job.first / 4u + 1u);
 #pragma unroll
-        for (uint32_t i = 0; i < BUFFERS; i++) copy(i);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((BUFFERS - 1) * COPIES) : "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        Scales now;
-        read_scales(now, 0);
-        read(held[0], 0, 0);
+        for (uint32_t i = 0; i < BUFFERS; i++)
+#pragma unroll
+            for (int q = 0; q < (int)COPIES; q++) copy(i, q);
+        landed(Number<(BUFFERS - 1) * COPIES>{});
+        Scales words;
+        read_scales(words, 0);
+#pragma unroll
+        for (int q = 0; q < TM + TN; q++) read(held[0], 0, 0, q);
         for (uint32_t s = 0; s < stages; s++) {
-            read(held[1], s, 1);
-            products<EXACT, TM, TN>(acc, held[0].x, now.x, held[0].y, now.y);
-            ready();
-            // the words after those that the next stage begins, into the place of some that nobody reads any more
-            if ((job.first + s + 1u) % 4u == 0) copy_scales((job.first + s + 1u) / 4u + 1u);
-            copy(s + BUFFERS);
-            read(held[0], s + 1, 0);
-            products<EXACT, TM, TN>(acc, held[1].x, now.x, held[1].y, now.y);
-            read_scales(now, s + 1);
+            held_back();
+            const Scales now = bytes_of(words, s);
+#pragma unroll
+            for (int q = 0; q < TM + TN; q++) read(held[1], s, 1, q);
+            products<EXACT, 0, N - PART>(acc, held[0].x, now.x, held[0].y, now.y);
+            if (!EXACT) mixed<N - PART, READS, 0>();
+            all_read();
+            // words that the next stages begin, into the place of some that nobody reads any more
+            if ((job.first + s) % 4u == 0) copy_scales((job.first + s) / 4u + 1u);
+#pragma unroll
+            for (int i = 0; i < CUT; i++) copy(s + BUFFERS, i);
+            products<EXACT, N - PART, N>(acc, held[0].x, now.x, held[0].y, now.y);
+            products<EXACT, 0, PART>(acc, held[1].x, now.x, held[1].y, now.y);
+            if (!EXACT) mixed<2 * PART, 0, CUT>();
+            landed(Number<(BUFFERS - 2) * COPIES + CUT>{});
+            read_scales(words, s + 1);
+#pragma unroll
+            for (int i = 0; i < (int)COPIES - CUT || i < TM + TN; i++) {
+                if (i < TM + TN) read(held[0], s + 1, 0, i);
+                if (CUT + i < (int)COPIES) copy(s + BUFFERS, CUT + i);
+            }
+            products<EXACT, PART, N>(acc, held[1].x, now.x, held[1].y, now.y);
+            if (!EXACT) {
+                mixed<1, (TM + TN) / 2, 0>();   // the words
+                mixed<N - PART - 1, READS, COPIES - CUT>();
+            }
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy outlives the workgroup's LDS
     }
@@ -376,6 +438,7 @@ hipError_t launch_f8_matmul(const F8MatmulArgs &a, uint32_t dtype, hipStream_t s
         typedef decltype(t) T;
         constexpr bool EXACT = sizeof(T) == 4;
         const uint32_t mt = (uint32_t)((a.m + 127) / 128), blocks = (uint32_t)f8_blocks(a.k), per = blocks_each(a.m, a.n, a.k);
+        if (tiles_of(a.m, a.n) >= 512) return product<T, EXACT, DENSE, 256, 256, 2, 2, 2>(a, (mt + 1) / 2, 1, blocks + 1, s);
         if (per >= blocks) return product<T, EXACT, DENSE, 128, 128, 2, 2, 4>(a, mt, 1, per, s);
         F8MatmulArgs part = a;
         part.out = a.part;
@@ -394,6 +457,7 @@ hipError_t launch_f8_expert_matmul(const F8MatmulArgs &a, uint32_t dtype, hipStr
 {
     return by_type(dtype, [&](auto t) -> hipError_t {
         typedef decltype(t) T;
+        if (a.rows / a.experts >= 256) return product<T, sizeof(T) == 4, EXPERTS, 256, 256, 2, 2, 2>(a, (uint32_t)groups_blocks(a.experts, a.rows, 256), 1, 0, s);
         return product<T, sizeof(T) == 4, EXPERTS, 128, 128, 2, 2, 4>(a, (uint32_t)groups_blocks(a.experts, a.rows, 128), 1, 0, s);
     });
 }

@@ -135,10 +135,10 @@ inline __host__ __device__ uint64_t f8_scale_bytes(uint64_t cols) { return (f8_b
 constexpr uint64_t F8_MAX_K = 1ull << 23;
 
 // Rows in expert order, cut into blocks of up to 128 rows of one expert (and of
-// up to 256, for larger tiles).  The table, in words: experts + 1 numbers of
-// blocks before each expert, then two words a block (its first row; its expert
-// and rows, expert | rows << 16), no rows in those that are not used; then the
-// larger blocks the same way.
+// up to 256, for larger tiles).  The table, in words: the numbers of blocks
+// before each expert and of all, the number of larger blocks, then two words a
+// block (its first row; its expert and rows, expert | rows << 16), no rows in
+// those that are not used; then the larger blocks the same way.
 inline __host__ __device__ uint64_t groups_blocks(uint64_t experts, uint64_t rows, uint32_t block)
 {
     return rows / block + (experts < rows ? experts : rows);
@@ -152,7 +152,7 @@ struct GroupsArgs {
 };
 inline __host__ __device__ uint64_t groups_words(uint64_t experts, uint64_t rows)
 {
-    return experts + 1 + 2 * groups_blocks(experts, rows, 128) + 2 * groups_blocks(experts, rows, 256);
+    return experts + 2 + 2 * groups_blocks(experts, rows, 128) + 2 * groups_blocks(experts, rows, 256);
 }
 hipError_t launch_groups(const GroupsArgs &a, hipStream_t s);
 

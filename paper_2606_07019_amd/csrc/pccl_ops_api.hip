@@ -334,7 +334,7 @@ pccl_status pccl_moe_groups(pccl_ctx *c, const int32_t *counts, uint32_t experts
         TRY(check_experts(c, experts, rows));
         NEED(counts && aligned(counts, 4), "counts are null or misaligned");
         NEED(groups && aligned(groups, 4), "groups are null or misaligned");
-        static_assert(PCCL_GROUP_WORDS(7, 1000) == 7 + 1 + 2 * (7 + 7) + 2 * (3 + 7), "the header's number of words");
+        static_assert(PCCL_GROUP_WORDS(7, 1000) == 7 + 2 + 2 * (7 + 7) + 2 * (3 + 7), "the header's number of words");
         OnDevice device;
         TRY(device.enter(c));
         const GroupsArgs a{counts, rows, experts, 0, groups_blocks(experts, rows, 128), groups_blocks(experts, rows, 256), groups};

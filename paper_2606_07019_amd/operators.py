@@ -84,6 +84,10 @@ def group_blocks(experts: int, rows: int, block: int = 128):
     return rows // block + min(experts, rows)
 
 
+def _group_words(experts, rows):
+    return experts + 2 + 2 * group_blocks(experts, rows) + 2 * group_blocks(experts, rows, 256)
+
+
 def _learns(*tensors):
     """Whether a derivative is recorded for one of the tensors; RuntimeError for a forward-mode one, which none has here."""
     if forward_ad._current_level >= 0 and any(forward_ad.unpack_dual(t).tangent is not None for t in tensors):
@@ -206,8 +210,7 @@ class Operators:
 
     def _blocks(self, groups: Groups):
         _, experts, rows = groups
-        words = experts + 1 + 2 * group_blocks(experts, rows) + 2 * group_blocks(experts, rows, 256)
-        return self._same("groups", groups.table, (words,), torch.int32)
+        return self._same("groups", groups.table, (_group_words(experts, rows),), torch.int32)
 
     def _result(self, out, rows, cols, dtype):
         """(out, its row stride): what a product is written to, made here or given by the caller."""
@@ -469,7 +472,7 @@ class Operators:
         cp = self._same("counts", counts, (experts,), torch.int32)
         if rows < 0:
             raise ValueError(f"{rows} rows")
-        table = self._empty(torch.int32, experts + 1 + 2 * group_blocks(experts, rows) + 2 * group_blocks(experts, rows, 256))
+        table = self._empty(torch.int32, _group_words(experts, rows))
         self._call(self._lib.pccl_moe_groups, cp, experts, rows, table.data_ptr(), self._stream())
         return Groups(table, experts, rows)
 

@@ -146,7 +146,8 @@ def test_groups(ops, counts, rows):
     t = _torch()
     g = ops.expert_groups(t.tensor(counts, dtype=t.int32, device="cuda"), rows)
     table, e = g.table.cpu().numpy(), len(counts)
-    at = e + 1
+    at = e + 2
+    assert table[e + 1] == len(O.expert_blocks(counts, rows, 256)[1])
     for block in (128, 256):
         starts, want = O.expert_blocks(counts, rows, block)
         if block == 128:
