@@ -114,6 +114,22 @@ struct Number {
     static constexpr int value = N;
 };
 
+// f(Number<0>{}), ... f(Number<N - 1>{})
+template <int N>
+struct Each {
+    template <class F>
+    static __device__ inline void run(F &&f)
+    {
+        Each<N - 1>::run(f);
+        f(Number<N - 1>{});
+    }
+};
+template <>
+struct Each<0> {
+    template <class F>
+    static __device__ inline void run(F &&) {}
+};
+
 // What a workgroup multiplies.
 enum Kind { DENSE, EXPERTS, GRADIENT };
 struct Job {
@@ -219,11 +235,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
         offb[i] = (row < ln ? row : ln) * cb + chunk;
     }
     const uint32_t stages = job.blocks, last = stages - 1u;
-    auto copy = [&](uint32_t stage, int i) {   // past the last stage: that one again, into a buffer nobody reads
-        const uint32_t k = (job.first + (stage < last ? stage : last)) * 128u;
+    auto copy = [&](uint32_t stage, int i) {   // past the last stage: one piece of its first row, into a buffer nobody reads
+        const uint32_t k = (job.first + (stage < last ? stage : last)) * 128u, keep = stage <= last ? ~0u : 0u;
         uint8_t *to = lds + stage % BUFFERS * STAGE + (i * THREADS + wave * 64u) * 16u;
-        if (i < PA) __builtin_amdgcn_global_load_lds((gptr)(job.a + (offa[i] + k)), (lptr)to, 16, 0, 0);
-        else __builtin_amdgcn_global_load_lds((gptr)(job.b + (offb[i - PA] + k)), (lptr)to, 16, 0, 0);
+        if (i < PA) __builtin_amdgcn_global_load_lds((gptr)(job.a + ((offa[i] & keep) + k)), (lptr)to, 16, 0, 0);
+        else __builtin_amdgcn_global_load_lds((gptr)(job.b + ((offb[i - PA] & keep) + k)), (lptr)to, 16, 0, 0);
     };
     // the scales of blocks 4 w ... + 3, a word of every row; a wave's rows are one operand's
     uint32_t offs[SCALES];
@@ -336,7 +352,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy outlives the workgroup's LDS
     }
-    // The sums go through LDS, 32 rows of the wave's at a time, so that whole rows of them are stored.
+    // The sums go through LDS, 32 rows of the wave's at a time, so that whole rows
+    // of them are stored, past the caches that the operands are read from (8192^3
+    // 445 us with ordinary stores, 433 with these; the gradient of 61 experts, 1000 x
+    // 2040 of f32, 243 and 167).
+    typedef u32x4 Chunk __attribute__((aligned(2)));   // at any address
     T *out = static_cast<T *>(a.out) + (KIND == EXPERTS ? 0u : (uint64_t)job.slice * a.m * a.ld);
     constexpr uint32_t COLS = BN / WN, EACH = 16 / sizeof(T), CHUNKS_ROW = COLS / EACH, ROW = COLS * sizeof(T) + 16;
     static_assert(WM * WN * 32 * ROW <= ALL, "within the stages' room");
@@ -362,7 +382,9 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
             __builtin_memcpy(t, __builtin_assume_aligned(own + row * ROW + col * sizeof(T), 16), 16);
             T *to = out + (job.row + m) * a.ld + job.col + n;
             if (n + EACH <= job.rows_b) {
-                __builtin_memcpy(to, t, 16);   // at any address
+                Chunk w;
+                __builtin_memcpy(&w, t, 16);
+                __builtin_nontemporal_store(w, reinterpret_cast<Chunk *>(to));
                 continue;
             }
 #pragma unroll
@@ -370,6 +392,162 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
                 if (n + c < job.rows_b) to[c] = t[c];
         }
     }
+}
+
+// ---- few rows ----------------------------------------------------------------
+
+// Sixteen rows of each operand over 128 values of k: lane l has 32 values of row
+// l % 16, and gets four neighbouring sums, rows 4 (l / 16) ... of y, row l % 16 of x.
+template <bool EXACT>
+__device__ inline f32x4 product16(const Piece &y, uint32_t ys, const Piece &x, uint32_t xs, f32x4 c)
+{
+    if constexpr (EXACT) {
+        const float fy = mx_scale(ys), fx = mx_scale(xs);
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const u32x4 &v = q < 2 ? y.lo : y.hi, &w = q < 2 ? x.lo : x.hi;
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide(v[q % 2 * 2], v[q % 2 * 2 + 1], fy), wide(w[q % 2 * 2], w[q % 2 * 2 + 1], fx), c, 0, 0, 0);
+        }
+        return c;
+    } else {
+        auto whole = [](const Piece &p) { return i32x8{(int)p.lo.x, (int)p.lo.y, (int)p.lo.z, (int)p.lo.w, (int)p.hi.x, (int)p.hi.y, (int)p.hi.z, (int)p.hi.w}; };
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(y), whole(x), c, 0, 0, 0, (int)ys, 0, (int)xs);
+    }
+}
+
+// Four neighbouring sums of row `row`, in the output's type.
+__device__ inline void store4_as(void *out, uint32_t dtype, uint64_t ld, uint64_t row, uint64_t col, uint64_t n, f32x4 v, bool vec)
+{
+    if (dtype == DT_F32) store4(static_cast<float *>(out), ld, row, col, n, v, vec);
+    else if (dtype == DT_BF16) store4(static_cast<__bf16 *>(out), ld, row, col, n, v, vec);
+    else store4(static_cast<_Float16 *>(out), ld, row, col, n, v, vec);
+}
+
+constexpr uint32_t SLOT = 2048 + 256;   // a step of 16 rows, and the words of their scales
+
+template <int MT, int WAVES, int D>
+constexpr uint32_t few_lds() { return WAVES * D * SLOT + 2 * WAVES * MT * 1024; }
+
+// Up to 16 MT rows of A: bound by reading B once.  The waves of a workgroup share
+// out its part of k, S steps of 128 values each, and hold A's operands of their
+// steps in registers; the workgroup goes through tiles of 16 rows of B.  A wave's
+// operands come straight to LDS in whole pieces of 128 bytes a row, D steps ahead
+// in a ring of its own, so that nothing is between the waves but the joining of
+// their sums, in their order.  Whoever has no more to read reads one piece, so
+// that as many copies are under way.
+template <bool EXACT, int MT, int S, int WAVES, int D>
+__global__ __launch_bounds__(64 * WAVES) void k_f8_few(F8MatmulArgs a, uint32_t dtype, bool vec, uint32_t tiles)
+{
+    extern __shared__ __align__(16) uint8_t lds[];
+    const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint32_t r = lane & 15u, g = lane >> 4;
+    const uint32_t cb = (uint32_t)f8_code_bytes(a.k), sb = (uint32_t)f8_scale_bytes(a.k), steps = (uint32_t)f8_blocks(a.k);
+    const uint32_t s0 = (blockIdx.y * WAVES + wave) * S, mine = s0 < steps ? (steps - s0 < S ? steps - s0 : S) : 0u;
+    const uint32_t rows = (uint32_t)a.m, mts = (rows + 15u) / 16u;
+    char *out = static_cast<char *>(a.out) + (uint64_t)blockIdx.y * a.m * a.ld * sizeof(float);   // of the partial sums
+    uint8_t *ring = lds + wave * (D * SLOT);
+    f32x4 *sums = reinterpret_cast<f32x4 *>(lds + WAVES * D * SLOT);   // [2][WAVES][MT][64]
+    const uint32_t mine_tiles = (tiles - blockIdx.x + gridDim.x - 1) / gridDim.x;
+
+    // where a lane's pieces and word of a whole tile lie: an instruction takes eight rows
+    const uint32_t chunk = lane / 16u * 16u, word = (s0 / 4u + g) * 4u < sb ? (s0 / 4u + g) * 4u : sb - 4u;
+    auto piece_of = [&](uint32_t i, uint32_t last) {
+        const uint32_t in = i * 8u + lane / 8u;
+        return (in < last ? in : last) * cb + ((lane % 8u * 16u) ^ ((i * 64u + chunk) & 112u));
+    };
+    auto word_of = [&](uint32_t last) { return (r < last ? r : last) * sb + word; };
+    const uint32_t piece[2] = {piece_of(0, 15), piece_of(1, 15)}, words = word_of(15);
+    // step j of the 16 rows at `first` of the `n` of an operand
+    auto issue = [&](const uint8_t *codes, const uint8_t *scales, uint64_t first, uint64_t n, int j, uint32_t slot) {
+        const bool some = (uint32_t)j < mine && first < n;
+        const uint32_t keep = some ? ~0u : 0u;
+        uint32_t off[2] = {piece[0], piece[1]}, at = words;
+        if (some && n - first < 16u) {   // rows past the last: that one again
+            const uint32_t last = (uint32_t)(n - first) - 1u;
+            off[0] = piece_of(0, last), off[1] = piece_of(1, last), at = word_of(last);
+        }
+        const uint8_t *from = some ? codes + first * cb + (s0 + j) * 128u : codes;
+        uint8_t *to = ring + slot * SLOT;
+#pragma unroll
+        for (uint32_t i = 0; i < 2; i++) __builtin_amdgcn_global_load_lds((gptr)(from + (off[i] & keep)), (lptr)(to + i * 1024u), 16, 0, 0);
+        // words s0 / 4 ... + 3 of the rows' scales
+        if (j == 0) __builtin_amdgcn_global_load_lds((gptr)((some ? scales + first * sb : scales) + (at & keep)), (lptr)(to + 2048u), 4, 0, 0);
+    };
+    auto issue_a = [&](int t, int j, uint32_t slot) { issue(a.a, a.as, (uint64_t)t * 16u, rows, j, slot); };
+    auto issue_b = [&](uint32_t i, int j, uint32_t slot) { issue(a.b, a.bs, ((uint64_t)blockIdx.x + (uint64_t)i * gridDim.x) * 16u, a.n, j, slot); };
+    uint32_t slot = 0;
+    auto next = [&]() { slot = slot + 1 == D ? 0 : slot + 1; };
+    auto landed = [&](auto step) {   // this one, of the D under way
+        constexpr int j = decltype(step)::value;
+        constexpr int begun = (j + D - 1) / S - j / S;   // tiles that begin among the later ones
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (D - 1) + begun) : "memory");
+    };
+    auto codes_of = [&]() {
+        const uint8_t *from = ring + slot * SLOT + r * 128u;
+        return Piece{*reinterpret_cast<const u32x4 *>(from + ((2u * g) ^ (r / 2u)) * 16u), *reinterpret_cast<const u32x4 *>(from + ((2u * g + 1u) ^ (r / 2u)) * 16u)};
+    };
+    auto scales_of = [&](uint32_t (&to)[S]) {
+        const uint8_t *from = ring + slot * SLOT + 2048u + r * 4u;
+#pragma unroll
+        for (uint32_t j = 0; j < S; j++) to[j] = from[((s0 + j) / 4u - s0 / 4u) * 64u + (s0 + j) % 4u];
+    };
+    // what has been read is in registers before its place is written to
+    auto taken = [&]() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+    Piece x[MT][S];
+    uint32_t xs[MT][S];
+#pragma unroll
+    for (int u = 0; u < D; u++) {
+        if (u / S < MT) issue_a(u / S, u % S, (uint32_t)u);
+        else issue_b((uint32_t)(u / S - MT), u % S, (uint32_t)u);
+    }
+#pragma unroll
+    for (int t = 0; t < MT; t++)
+        Each<S>::run([&](auto step) {
+            constexpr int j = decltype(step)::value;
+            landed(step);
+            if constexpr (j == 0) scales_of(xs[t]);
+            x[t][j] = codes_of();
+            taken();
+            if (t + (j + D) / S < MT) issue_a(t + (j + D) / S, (j + D) % S, slot);
+            else issue_b((uint32_t)(t + (j + D) / S - MT), (j + D) % S, slot);
+            next();
+        });
+    for (uint32_t i = 0; i < mine_tiles; i++) {
+        f32x4 acc[MT] = {};
+        uint32_t ys[S];
+        Each<S>::run([&](auto step) {
+            constexpr int j = decltype(step)::value;
+            landed(step);
+            if constexpr (j == 0) scales_of(ys);
+            const Piece y = codes_of();
+            taken();
+            issue_b(i + (uint32_t)((j + D) / S), (j + D) % S, slot);
+            next();
+            if ((uint32_t)j < mine) {
+#pragma unroll
+                for (int t = 0; t < MT; t++)
+                    if ((uint32_t)t < mts) {
+                        // as codes, not as the twice as many registers of bf16 that they become anew for every tile
+                        if constexpr (EXACT) asm volatile("" : "+v"(x[t][j].lo), "+v"(x[t][j].hi));
+                        acc[t] = product16<EXACT>(y, ys[j], x[t][j], xs[t][j], acc[t]);
+                    }
+            }
+        });
+        f32x4 *part = sums + (i % 2u) * (WAVES * MT * 64u);
+#pragma unroll
+        for (int t = 0; t < MT; t++) part[(wave * MT + t) * 64u + lane] = acc[t];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();   // the sums of the tile before last have been read by then
+        asm volatile("" ::: "memory");
+        if (wave < MT) {
+            f32x4 v = part[wave * 64u + lane];
+#pragma unroll
+            for (uint32_t q = 1; q < WAVES; q++) v += part[(q * MT + wave) * 64u + lane];
+            const uint32_t m = wave * 16u + r;
+            if (m < rows) store4_as(out, dtype, a.ld, m, ((uint64_t)blockIdx.x + (uint64_t)i * gridDim.x) * 16u + g * 4u, a.n, v, vec);
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy outlives the workgroup's LDS
 }
 
 // The sums of a shared-out k, joined in the order of its parts: a thread takes
@@ -405,30 +583,106 @@ hipError_t by_type(uint32_t dtype, F &&f)
     return f(_Float16{});
 }
 
-inline uint64_t tiles_of(uint64_t m, uint64_t n) { return ((m + 127) / 128) * ((n + 127) / 128); }
+inline uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t side = 128) { return ((m + side - 1) / side) * ((n + side - 1) / side); }
 
-// Blocks of k that a workgroup takes: all, or, where tiles are too few for 256
-// compute units, parts of sixteen blocks (2048 values) or more.
-constexpr uint32_t LEAST_BLOCKS = 16;
-inline uint32_t blocks_each(uint64_t m, uint64_t n, uint64_t k)
+// Tiles of 256 x 256 or of 128 x 128, by rounds over 256 compute units.  A round
+// of the larger ones takes as long as three of the smaller ones (with k = 2048, in
+// us, large and small: 128 and 512 tiles 28 and 23, 160 and 640 28 and 31, 256 and
+// 1024 34 and 44, 272 and 1088 53 and 52, 384 and 1536 58 and 64), or, with
+// results of 32 bits, as three and a half (47 and 36, 47 and 46, 63 and 67, 100
+// and 77, 103 and 98).
+inline bool large_tiles(uint64_t small, uint64_t large, bool exact)
 {
-    const uint64_t blocks = f8_blocks(k), tiles = tiles_of(m, n), want = tiles < 256 ? 256 / tiles : 1;
+    const uint64_t s = (small + 255) / 256, l = (large + 255) / 256;
+    return exact ? 2 * s >= 7 * l : s >= 3 * l;
+}
+
+// How a product is made: k in `parts` of `per` blocks; few rows with steps of
+// `each` a wave.
+constexpr uint32_t FEW_ROWS = 64;
+constexpr int FEW_WAVES = 8, FEW_AHEAD = 4;   // seven steps ahead take as long as four
+constexpr uint32_t LEAST_BLOCKS = 16;
+struct Plan {
+    bool few;
+    uint32_t parts, per, each;
+};
+// steps that a wave can hold of so many sixteens of rows
+inline uint32_t most_steps(uint32_t mt) { return mt == 1 ? 8u : mt == 2 ? 8u : mt == 3 ? 5u : 4u; }
+
+inline Plan plan(uint64_t m, uint64_t n, uint64_t k)
+{
+    const uint32_t blocks = (uint32_t)f8_blocks(k);
+    Plan p{m <= FEW_ROWS && blocks > 0, 1, 0, 0};
+    if (p.few) {
+        const uint32_t mt = (uint32_t)(m + 15) / 16, most = most_steps(mt);
+        p.parts = (blocks + FEW_WAVES * most - 1) / (FEW_WAVES * most);
+        p.each = (blocks + FEW_WAVES * p.parts - 1) / (FEW_WAVES * p.parts);
+        p.per = p.each * FEW_WAVES;
+        return p;
+    }
+    // Blocks of k that a workgroup takes: all, or, where tiles are too few for 256
+    // compute units, parts of sixteen blocks (2048 values) or more.
+    const uint64_t tiles = tiles_of(m, n), want = tiles < 256 ? 256 / tiles : 1;
     uint64_t per = (blocks + want - 1) / want;
     if (per < LEAST_BLOCKS) per = LEAST_BLOCKS;
-    return (uint32_t)(per < blocks ? per : blocks + (blocks == 0));
+    if (per >= blocks) {
+        p.per = blocks + 1;
+        return p;
+    }
+    p.per = (uint32_t)per;
+    p.parts = (uint32_t)((blocks + per - 1) / per);
+    return p;
 }
 inline uint64_t padded(uint64_t n) { return (n + 3) / 4 * 4; }
+
+template <bool EXACT, int MT, int S, int WAVES, int D>
+hipError_t few_as(const F8MatmulArgs &a, uint32_t dtype, uint32_t slices, uint32_t workers, hipStream_t s)
+{
+    constexpr uint32_t bytes = few_lds<MT, WAVES, D>();
+    static_assert(bytes <= 160u << 10 && MT * S <= 16, "one workgroup's LDS, and registers");
+    const hipError_t e = allow_lds<&k_f8_few<EXACT, MT, S, WAVES, D>>(bytes);
+    if (e != hipSuccess) return e;
+    const size_t elem = dtype == DT_F32 ? 4 : 2;
+    const bool vec = (reinterpret_cast<uintptr_t>(a.out) | (a.ld * elem)) % (4 * elem) == 0;
+    const uint32_t tiles = (uint32_t)((a.n + 15) / 16);
+    k_f8_few<EXACT, MT, S, WAVES, D><<<dim3(tiles < workers ? tiles : workers, slices), 64 * WAVES, bytes, s>>>(a, dtype, vec, tiles);
+    return hipGetLastError();
+}
+
+template <bool EXACT, int MT>
+hipError_t few_rows(const F8MatmulArgs &a, uint32_t dtype, const Plan &p, hipStream_t s)
+{
+    const uint32_t workers = (256 + p.parts - 1) / p.parts;   // one a compute unit
+#define STEPS(S)                                                                                             \
+    if constexpr (MT * S <= 16)                                                                              \
+        if (p.each <= S) return few_as<EXACT, MT, S, FEW_WAVES, FEW_AHEAD>(a, dtype, p.parts, workers, s);
+    STEPS(1) STEPS(2) STEPS(3) STEPS(4) STEPS(5) STEPS(6) STEPS(8)
+#undef STEPS
+    return hipErrorInvalidValue;   // not reached: most_steps()
+}
+
+template <class T>
+hipError_t join(const F8MatmulArgs &a, uint32_t parts, hipStream_t s)
+{
+    const uint64_t ld = padded(a.n), threads = a.m * (ld / 4);
+    const bool vec = (reinterpret_cast<uintptr_t>(a.out) | (a.ld * sizeof(T))) % (4 * sizeof(T)) == 0;
+    k_f8_join<T><<<dim3((uint32_t)((threads + 255) / 256)), 256, 0, s>>>(a, parts, ld, vec);
+    return hipGetLastError();
+}
 
 }  // namespace
 
 size_t f8_matmul_workspace(uint64_t m, uint64_t n, uint64_t k)
 {
-    const uint64_t blocks = f8_blocks(k), per = blocks_each(m, n, k);
-    if (per >= blocks) return 0;
-    return (size_t)((blocks + per - 1) / per * m * padded(n) * sizeof(float));
+    const Plan p = plan(m, n, k);
+    return p.parts > 1 ? (size_t)(p.parts * m * padded(n) * sizeof(float)) : 0;
 }
 
-bool f8_matmul_fits(uint64_t m, uint64_t n, uint64_t) { return tiles_of(m, n) <= most_blocks(256); }
+bool f8_matmul_fits(uint64_t m, uint64_t n, uint64_t k)
+{
+    const Plan p = plan(m, n, k);
+    return p.few ? p.parts == 1 || m * (padded(n) / 4) <= most_blocks(256) * 256 : tiles_of(m, n) <= most_blocks(256);
+}
 bool f8_experts_fit(uint64_t rows, uint32_t experts, uint64_t n) { return groups_blocks(experts, rows, 128) * ((n + 127) / 128) <= most_blocks(256); }
 bool f8_gradients_fit(uint32_t experts, uint64_t m, uint64_t n) { return tiles_of(m, n) <= most_blocks(256) / experts; }
 
@@ -437,19 +691,30 @@ hipError_t launch_f8_matmul(const F8MatmulArgs &a, uint32_t dtype, hipStream_t s
     return by_type(dtype, [&](auto t) -> hipError_t {
         typedef decltype(t) T;
         constexpr bool EXACT = sizeof(T) == 4;
-        const uint32_t mt = (uint32_t)((a.m + 127) / 128), blocks = (uint32_t)f8_blocks(a.k), per = blocks_each(a.m, a.n, a.k);
-        if (tiles_of(a.m, a.n) >= 512) return product<T, EXACT, DENSE, 256, 256, 2, 2, 2>(a, (mt + 1) / 2, 1, blocks + 1, s);
-        if (per >= blocks) return product<T, EXACT, DENSE, 128, 128, 2, 2, 4>(a, mt, 1, per, s);
+        const Plan p = plan(a.m, a.n, a.k);
+        const uint32_t mt = (uint32_t)((a.m + 127) / 128);
         F8MatmulArgs part = a;
-        part.out = a.part;
-        part.ld = padded(a.n);
-        const uint32_t splits = (blocks + per - 1) / per;
-        const hipError_t e = product<float, EXACT, DENSE, 128, 128, 2, 2, 4>(part, mt, splits, per, s);
-        if (e != hipSuccess) return e;
-        const uint64_t threads = a.m * (part.ld / 4);
-        const bool vec = (reinterpret_cast<uintptr_t>(a.out) | (a.ld * sizeof(T))) % (4 * sizeof(T)) == 0;
-        k_f8_join<T><<<dim3((uint32_t)((threads + 255) / 256)), 256, 0, s>>>(a, splits, part.ld, vec);
-        return hipGetLastError();
+        if (p.parts > 1) {
+            part.out = a.part;
+            part.ld = padded(a.n);
+        }
+        hipError_t e;
+        if (p.few) {
+            const uint32_t type = p.parts > 1 ? (uint32_t)DT_F32 : dtype;
+            if (a.m <= 16) e = few_rows<EXACT, 1>(part, type, p, s);
+            else if (a.m <= 32) e = few_rows<EXACT, 2>(part, type, p, s);
+            else if (a.m <= 48) e = few_rows<EXACT, 3>(part, type, p, s);
+            else e = few_rows<EXACT, 4>(part, type, p, s);
+        } else if (p.parts > 1) {
+            e = product<float, EXACT, DENSE, 128, 128, 2, 2, 4>(part, mt, p.parts, p.per, s);
+        } else if (large_tiles(tiles_of(a.m, a.n), tiles_of(a.m, a.n, 256), EXACT)) {
+            e = product<T, EXACT, DENSE, 256, 256, 2, 2, 2>(a, (mt + 1) / 2, 1, p.per, s);
+        } else if (tiles_of(a.m, a.n) > 256) {   // two workgroups a compute unit, with half as much copied ahead (2048^2 x 8192, one tile each, 44 and 50 us; 2080 x 2040 x 1500, 272 tiles, 20 and 15)
+            e = product<T, EXACT, DENSE, 128, 128, 2, 2, 2>(a, mt, 1, p.per, s);
+        } else {
+            e = product<T, EXACT, DENSE, 128, 128, 2, 2, 4>(a, mt, 1, p.per, s);
+        }
+        return e == hipSuccess && p.parts > 1 ? join<T>(a, p.parts, s) : e;
     });
 }
 
@@ -457,8 +722,12 @@ hipError_t launch_f8_expert_matmul(const F8MatmulArgs &a, uint32_t dtype, hipStr
 {
     return by_type(dtype, [&](auto t) -> hipError_t {
         typedef decltype(t) T;
-        if (a.rows / a.experts >= 256) return product<T, sizeof(T) == 4, EXPERTS, 256, 256, 2, 2, 2>(a, (uint32_t)groups_blocks(a.experts, a.rows, 256), 1, 0, s);
-        return product<T, sizeof(T) == 4, EXPERTS, 128, 128, 2, 2, 4>(a, (uint32_t)groups_blocks(a.experts, a.rows, 128), 1, 0, s);
+        constexpr bool EXACT = sizeof(T) == 4;
+        // an expert's last block is half full, as far as one can know here
+        const uint64_t half = a.experts / 2, small = (a.rows / 128 + half) * ((a.n + 127) / 128), large = (a.rows / 256 + half) * ((a.n + 255) / 256);
+        if (large_tiles(small, large, EXACT))
+            return product<T, EXACT, EXPERTS, 256, 256, 2, 2, 2>(a, (uint32_t)groups_blocks(a.experts, a.rows, 256), 1, 0, s);
+        return product<T, EXACT, EXPERTS, 128, 128, 2, 2, 2>(a, (uint32_t)groups_blocks(a.experts, a.rows, 128), 1, 0, s);
     });
 }
 
@@ -466,7 +735,10 @@ hipError_t launch_f8_expert_gradient(const F8MatmulArgs &a, uint32_t dtype, hipS
 {
     return by_type(dtype, [&](auto t) -> hipError_t {
         typedef decltype(t) T;
-        return product<T, sizeof(T) == 4, GRADIENT, 128, 128, 2, 2, 4>(a, (uint32_t)((a.m + 127) / 128), a.experts, 0, s);
+        constexpr bool EXACT = sizeof(T) == 4;
+        if (large_tiles(a.experts * tiles_of(a.m, a.n), a.experts * tiles_of(a.m, a.n, 256), EXACT))
+            return product<T, EXACT, GRADIENT, 256, 256, 2, 2, 2>(a, (uint32_t)((a.m + 255) / 256), a.experts, 0, s);
+        return product<T, EXACT, GRADIENT, 128, 128, 2, 2, 2>(a, (uint32_t)((a.m + 127) / 128), a.experts, 0, s);
     });
 }
 
