@@ -13,46 +13,67 @@
 namespace pccl {
 namespace {
 
-constexpr int THREADS = 256, WAVES = 4;
-constexpr uint32_t MOST_GROUPS = 512;   // workgroups that the rows are shared out to
-constexpr uint32_t JOIN_EXPERTS = 16;   // experts of a joining workgroup
+constexpr int THREADS = 1024, WAVES = 16;   // of the forward pass
+constexpr uint32_t MOST_GROUPS = 256;        // workgroups that the rows are shared out to
+constexpr uint32_t JOIN_EXPERTS = 16;        // experts of a joining workgroup
 
-template <class T, int V>
-__device__ inline void load_row(const T *row, uint32_t experts, uint32_t sub, bool vec, T (&t)[V])
-{
-    const uint32_t e0 = sub * V;
-    if (vec && e0 + V <= experts) {
-        __builtin_memcpy(t, __builtin_assume_aligned(row + e0, sizeof t < 16 ? sizeof t : 16), sizeof t);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < V; i++) t[i] = e0 + i < experts ? row[e0 + i] : (T)0.f;
-}
-
-// A row's softmax in place of its logits: v and, as the result, whether the row
-// has an expert left (otherwise zeros).  A NaN or plus infinity makes the row's NaN.
+// The logits of a lane: V in pieces of up to 16 bytes, so that a row's lanes read
+// one neighbouring piece each.
 template <class T, int LANES, int V>
-__device__ inline bool softmax(const T (&t)[V], bool there, uint32_t experts, uint32_t sub, float (&v)[V])
-{
-    uint32_t key[V], most = 0;
+struct Share {
+    static constexpr int PIECE = V * sizeof(T) < 16 ? V : 16 / sizeof(T);
+    static __device__ uint32_t expert(uint32_t sub, int i) { return i / PIECE * (LANES * PIECE) + sub * PIECE + i % PIECE; }
+    static __device__ void load(const T *row, uint32_t experts, uint32_t sub, bool vec, T (&t)[V])
+    {
 #pragma unroll
-    for (int i = 0; i < V; i++) {
-        key[i] = there && sub * V + i < experts ? Key<float>::of(Elem<T>::get(t[i]), 0) : 0u;
-        most = key[i] > most ? key[i] : most;
+        for (int i = 0; i < V; i += PIECE) {
+            const uint32_t e = expert(sub, i);
+            if (vec && e + PIECE <= experts) {
+                __builtin_memcpy(t + i, __builtin_assume_aligned(row + e, PIECE * sizeof(T)), PIECE * sizeof(T));
+                continue;
+            }
+#pragma unroll
+            for (int j = 0; j < PIECE; j++) t[i + j] = e + j < experts ? row[e + j] : (T)-INFINITY;
+        }
     }
-    most = row_max<LANES>(most);
-    const bool any = most > Key<float>::EMPTY;
-    const float top = Key<float>::value(most);
+    static __device__ void store(T *row, uint32_t experts, uint32_t sub, bool vec, const T (&t)[V])
+    {
+#pragma unroll
+        for (int i = 0; i < V; i += PIECE) {
+            const uint32_t e = expert(sub, i);
+            if (vec && e + PIECE <= experts) {
+                __builtin_memcpy(__builtin_assume_aligned(row + e, PIECE * sizeof(T)), t + i, PIECE * sizeof(T));
+                continue;
+            }
+#pragma unroll
+            for (int j = 0; j < PIECE; j++)
+                if (e + j < experts) row[e + j] = t[i + j];
+        }
+    }
+};
+
+// A row's softmax: v and, as the result, whether the row has an expert left
+// (otherwise zeros).  Minus infinity is no expert; a NaN among the logits is lost
+// in the largest but not in the sum, and makes the row's NaN, as plus infinity does.
+template <class T, int LANES, int V>
+__device__ inline bool softmax(const T (&t)[V], bool there, float (&v)[V])
+{
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < V; i++) top = fmaxf(top, Elem<T>::get(t[i]));
+    top = Key<float>::value(row_max<LANES>(Key<float>::of(top, 0)));
+    top = there && top != -INFINITY ? top : 0.f;
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < V; i++) {
-        v[i] = any && key[i] > Key<float>::EMPTY ? expf(Elem<T>::get(t[i]) - top) : 0.f;
+        v[i] = expf(Elem<T>::get(t[i]) - top);
         sum += v[i];
     }
     sum = row_sum<LANES>(sum);
-    const float scale = any ? 1.f / sum : 0.f;
+    const bool any = there && sum != 0.f;   // its largest logit adds 1
+    const float scale = 1.f / sum;
 #pragma unroll
-    for (int i = 0; i < V; i++) v[i] *= scale;
+    for (int i = 0; i < V; i++) v[i] = any ? v[i] * scale : 0.f;
     return any;
 }
 
@@ -74,12 +95,39 @@ inline __host__ __device__ Space space_of(char *ws, uint32_t groups, uint32_t ex
     return s;
 }
 
+// Sums over the threads of a workgroup of N waves, in a fixed order; all get them.
+template <int N>
+__device__ inline void over_all(uint32_t &u, float &f, uint32_t *us, float *fs)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        u += (uint32_t)__shfl_xor((int)u, o);
+        f += __shfl_xor(f, o);
+    }
+    const uint32_t wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63u) == 0) {
+        us[wave] = u;
+        fs[wave] = f;
+    }
+    __syncthreads();
+    u = 0;
+    f = 0.f;
+#pragma unroll
+    for (int w = 0; w < N; w++) {
+        u += us[w];
+        f += fs[w];
+    }
+}
+
+// LANES lanes a row, WAVES * 64 / LANES rows at a time; the next ones are read
+// while these are summed up.
 template <class T, int LANES, int V>
 __global__ __launch_bounds__(THREADS) void k_balance(BalanceArgs a, bool vec)
 {
     constexpr int PER = 64 / LANES;   // rows of a wave at a time
+    constexpr uint32_t ROWS = WAVES * PER;
     __shared__ uint32_t hist[LANES * V], live[WAVES];
-    __shared__ float sums[WAVES * PER][LANES * V];
+    __shared__ float sums[WAVES / 2][LANES * V];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, sub = lane % LANES, mine = wave * PER + lane / LANES;
     for (uint32_t e = threadIdx.x; e < LANES * V; e += THREADS) hist[e] = 0;
     __syncthreads();
@@ -90,155 +138,244 @@ __global__ __launch_bounds__(THREADS) void k_balance(BalanceArgs a, bool vec)
     for (int i = 0; i < V; i++) acc[i] = 0.f;
     uint32_t rows = 0;
     const T *logits = static_cast<const T *>(a.logits);
-    for (uint64_t r0 = (uint64_t)blockIdx.x * (WAVES * PER); r0 < a.tokens; r0 += (uint64_t)gridDim.x * (WAVES * PER)) {
-        const uint64_t r = r0 + mine, row = r < a.tokens ? r : a.tokens - 1;
+    const uint64_t step = (uint64_t)gridDim.x * ROWS;
+    struct Row {
         T t[V];
-        load_row<T, V>(logits + row * a.ld, a.experts, sub, vec, t);
-        const bool there = r < a.tokens && (!a.mask || a.mask[row]);
+        bool there;
+        int32_t id;   // of a lane's first pick
+    } now, then;
+    auto load = [&](Row &to, uint64_t r) {
+        const uint64_t row = r < a.tokens ? r : a.tokens - 1;
+        Share<T, LANES, V>::load(logits + row * a.ld, a.experts, sub, vec, to.t);
+        to.there = r < a.tokens && (!a.mask || a.mask[row]);
+        to.id = sub < a.topk ? a.ids[row * a.topk + sub] : -1;
+    };
+    auto count = [&](int32_t id) {
+        if ((uint32_t)id < a.experts) atomicAdd(&hist[id], 1u);   // LDS; whole numbers
+    };
+    uint64_t r0 = (uint64_t)blockIdx.x * ROWS;
+    if (r0 < a.tokens) load(now, r0 + mine);
+    for (; r0 < a.tokens; r0 += step) {
+        if (r0 + step < a.tokens) load(then, r0 + step + mine);
         float v[V];
-        const bool any = softmax<T, LANES, V>(t, there, a.experts, sub, v);
+        const bool any = softmax<T, LANES, V>(now.t, now.there, v);
 #pragma unroll
         for (int i = 0; i < V; i++) acc[i] += v[i];
-        if (!any) continue;
-        rows += sub == 0;
-        for (uint32_t j = sub; j < a.topk; j += LANES) {
-            const uint32_t e = (uint32_t)a.ids[row * a.topk + j];
-            if (e < a.experts) atomicAdd(&hist[e], 1u);   // LDS; whole numbers
+        if (any) {
+            rows += sub == 0;
+            count(now.id);
+            for (uint32_t j = sub + LANES; j < a.topk; j += LANES) count(a.ids[(r0 + mine) * a.topk + j]);
         }
+        now = then;
     }
+    // a wave's rows, then the upper half of the waves to the lower, then those
 #pragma unroll
-    for (int i = 0; i < V; i++) sums[mine][sub * V + i] = acc[i];
+    for (int i = 0; i < V; i++) {
+#pragma unroll
+        for (int o = LANES; o < 64; o <<= 1) acc[i] += __shfl_xor(acc[i], o);
+    }
+    if (wave >= WAVES / 2 && lane < LANES) {
+#pragma unroll
+        for (int i = 0; i < V; i++) sums[wave - WAVES / 2][Share<T, LANES, V>::expert(sub, i)] = acc[i];
+    }
+    __syncthreads();
+    if (wave < WAVES / 2 && lane < LANES) {
+#pragma unroll
+        for (int i = 0; i < V; i++) sums[wave][Share<T, LANES, V>::expert(sub, i)] += acc[i];
+    }
 #pragma unroll
     for (int o = 32; o; o >>= 1) rows += (uint32_t)__shfl_xor((int)rows, o);
     if (lane == 0) live[wave] = rows;
     __syncthreads();
     for (uint32_t e = threadIdx.x; e < a.experts; e += THREADS) {
-        float x = sums[0][e];
+        float x = 0.f;
 #pragma unroll
-        for (int w = 1; w < WAVES * PER; w++) x += sums[w][e];
+        for (uint32_t w = 0; w < WAVES / 2; w++) x += sums[w][e];
         s.probs[(uint64_t)blockIdx.x * a.experts + e] = x;
         s.counts[(uint64_t)blockIdx.x * a.experts + e] = hist[e];
     }
-    if (threadIdx.x == 0) s.rows[blockIdx.x] = live[0] + live[1] + live[2] + live[3];
-}
-
-// Adds up over the threads of a workgroup, in a fixed order; all get the result.
-template <class S>
-__device__ inline S over_all(S v, S *room)
-{
-    __syncthreads();
-    room[threadIdx.x] = v;
-    __syncthreads();
-    for (uint32_t o = THREADS / 2; o; o >>= 1) {
-        if (threadIdx.x < o) room[threadIdx.x] += room[threadIdx.x + o];
-        __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t all = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; w++) all += live[w];
+        s.rows[blockIdx.x] = all;
     }
-    return room[0];
 }
 
-// Sixteen experts a workgroup, sixteen threads an expert; the last one to be
-// done adds up the loss, whose factor 1 / sum of the counts is known only then.
-__global__ __launch_bounds__(THREADS) void k_balance_join(BalanceArgs a, uint32_t groups)
+// The workgroups' sums joined.  Few of them, and of experts: one workgroup, up to
+// LOADS of them a thread.
+constexpr uint32_t LOADS = 16;
+__global__ __launch_bounds__(THREADS) void k_balance_join(BalanceArgs a, uint32_t groups, uint32_t log_experts)
 {
-    __shared__ float fsum[THREADS];
-    __shared__ uint32_t usum[THREADS];
-    __shared__ uint32_t last;
+    __shared__ float fsum[THREADS], fs[WAVES];
+    __shared__ uint32_t usum[THREADS], us[WAVES];
     const Space s = space_of(a.ws, groups, a.experts);
-    const uint32_t e = blockIdx.x * JOIN_EXPERTS + threadIdx.x % JOIN_EXPERTS, part = threadIdx.x / JOIN_EXPERTS;
-    constexpr uint32_t PARTS = THREADS / JOIN_EXPERTS;
-    uint32_t rows = 0;
-    for (uint32_t g = threadIdx.x; g < groups; g += THREADS) rows += s.rows[g];
-    rows = over_all(rows, usum);
-    float p = 0.f;
-    uint32_t c = 0;
-    if (e < a.experts)
-        for (uint32_t g = part; g < groups; g += PARTS) {
-            p += s.probs[(uint64_t)g * a.experts + e];
-            c += s.counts[(uint64_t)g * a.experts + e];
-        }
+    const uint32_t e = threadIdx.x & ((1u << log_experts) - 1u), part = threadIdx.x >> log_experts, parts = THREADS >> log_experts;
+    float p = 0.f, zero = 0.f;
+    uint32_t c = 0, rows = threadIdx.x < groups ? s.rows[threadIdx.x] : 0u;
+#pragma unroll
+    for (uint32_t i = 0; i < LOADS; i++) {
+        const uint32_t g = part + i * parts;
+        const bool in = g < groups && e < a.experts;
+        p += in ? s.probs[(uint64_t)g * a.experts + e] : 0.f;
+        c += in ? s.counts[(uint64_t)g * a.experts + e] : 0u;
+    }
     fsum[threadIdx.x] = p;
-    __syncthreads();
     usum[threadIdx.x] = c;
-    __syncthreads();
-    if (part == 0) {
-        for (uint32_t j = 1; j < PARTS; j++) {
-            p += fsum[j * JOIN_EXPERTS + threadIdx.x];
-            c += usum[j * JOIN_EXPERTS + threadIdx.x];
+    over_all<WAVES>(rows, zero, us, fs);   // and a barrier
+    p = 0.f;
+    c = 0;
+    if (part == 0 && e < a.experts) {
+        for (uint32_t j = 0; j < parts; j++) {
+            p += fsum[(j << log_experts) + e];
+            c += usum[(j << log_experts) + e];
         }
         p = rows ? p / (float)rows : 0.f;
+        a.probs[e] = p;
+        a.counts[e] = (int32_t)c;
+    }
+    float loss = (float)c * p;
+    uint32_t picks = c;
+    __syncthreads();   // us and fs have been read
+    over_all<WAVES>(picks, loss, us, fs);
+    if (threadIdx.x == 0) {
+        *a.loss = picks ? loss * ((float)a.experts / (float)picks) : 0.f;
+        *a.rows = (int32_t)rows;
+    }
+}
+
+// Many: sixteen experts a workgroup, 64 threads an expert; the last one to be
+// done adds up the loss, whose factor 1 / sum of the counts is known only then.
+// What it reads of the others is written past the caches before they say that they
+// are done (a release of all that the caches hold takes 5 us more).
+__global__ __launch_bounds__(THREADS) void k_balance_join_many(BalanceArgs a, uint32_t groups)
+{
+    constexpr uint32_t PARTS = THREADS / JOIN_EXPERTS, MOST = MOST_GROUPS / PARTS;
+    static_assert(MOST_GROUPS <= THREADS && MOST_GROUPS % PARTS == 0, "a thread's share");
+    __shared__ float fsum[PARTS][JOIN_EXPERTS + 1], fs[WAVES];
+    __shared__ uint32_t usum[PARTS][JOIN_EXPERTS + 1], us[WAVES];
+    __shared__ uint32_t last;
+    const Space s = space_of(a.ws, groups, a.experts);
+    const uint32_t mine = threadIdx.x % JOIN_EXPERTS, e = blockIdx.x * JOIN_EXPERTS + mine, part = threadIdx.x / JOIN_EXPERTS;
+    float p[MOST], zero = 0.f;
+    uint32_t c[MOST], rows = threadIdx.x < groups ? s.rows[threadIdx.x] : 0u;
+#pragma unroll
+    for (uint32_t i = 0; i < MOST; i++) {
+        const uint32_t g = part + i * PARTS;
+        const bool in = g < groups && e < a.experts;
+        p[i] = in ? s.probs[(uint64_t)g * a.experts + e] : 0.f;
+        c[i] = in ? s.counts[(uint64_t)g * a.experts + e] : 0u;
+    }
+#pragma unroll
+    for (uint32_t i = 1; i < MOST; i++) {
+        p[0] += p[i];
+        c[0] += c[i];
+    }
+    fsum[part][mine] = p[0];
+    usum[part][mine] = c[0];
+    over_all<WAVES>(rows, zero, us, fs);   // and a barrier
+    if (part == 0) {
+        float sum = 0.f;
+        uint32_t n = 0;
+#pragma unroll 16
+        for (uint32_t j = 0; j < PARTS; j++) {
+            sum += fsum[j][mine];
+            n += usum[j][mine];
+        }
         if (e < a.experts) {
-            a.probs[e] = p;
-            a.counts[e] = (int32_t)c;
+            __hip_atomic_store(a.probs + e, rows ? sum / (float)rows : 0.f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(a.counts + e, (int32_t)n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.rows = (int32_t)rows;
-    __threadfence();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // those are there
     __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(s.done, 1u) + 1u == gridDim.x;
+    if (threadIdx.x == 0) last = __hip_atomic_fetch_add(s.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == gridDim.x;
     __syncthreads();
     if (!last) return;
-    __threadfence();
     uint32_t picks = 0;
-    for (uint32_t i = threadIdx.x; i < a.experts; i += THREADS) picks += __hip_atomic_load((uint32_t *)a.counts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    picks = over_all(picks, usum);
     float loss = 0.f;
     for (uint32_t i = threadIdx.x; i < a.experts; i += THREADS) {
-        const float n = (float)__hip_atomic_load((uint32_t *)a.counts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        loss += n * __hip_atomic_load(a.probs + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t n = (uint32_t)__hip_atomic_load(a.counts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        picks += n;
+        loss += (float)n * __hip_atomic_load(a.probs + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    loss = over_all(loss, fsum);
+    over_all<WAVES>(picks, loss, us, fs);
     if (threadIdx.x == 0) *a.loss = picks ? loss * ((float)a.experts / (float)picks) : 0.f;
 }
 
+constexpr int BACK_THREADS = 256, BACK_WAVES = 4;
+constexpr uint32_t BACK_GROUPS = 1024;   // workgroups at most
+
 template <class T, int LANES, int V>
-__global__ __launch_bounds__(THREADS) void k_balance_backward(BalanceBackwardArgs a, bool vec)
+__global__ __launch_bounds__(BACK_THREADS) void k_balance_backward(BalanceBackwardArgs a, bool vec)
 {
     constexpr int PER = 64 / LANES;
-    __shared__ uint32_t usum[THREADS];
+    constexpr uint32_t ROWS = BACK_WAVES * PER;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, sub = lane % LANES, mine = wave * PER + lane / LANES;
-    uint32_t picks = 0;
-    for (uint32_t i = threadIdx.x; i < a.experts; i += THREADS) picks += (uint32_t)a.counts[i];
-    picks = over_all(picks, usum);
-    const uint32_t rows = (uint32_t)*a.rows;
-    const float each = rows ? 1.f / (float)rows : 0.f;
-    const float unit = a.dloss && picks ? *a.dloss * ((float)a.experts / (float)picks) : 0.f;
-    float g[V];   // what the experts' probabilities are worth
-#pragma unroll
-    for (int i = 0; i < V; i++) {
-        const uint32_t e = sub * V + i;
-        g[i] = e < a.experts ? (unit * (float)a.counts[e] + (a.dprobs ? a.dprobs[e] : 0.f)) * each : 0.f;
-    }
     const T *logits = static_cast<const T *>(a.logits);
-    for (uint64_t r0 = (uint64_t)blockIdx.x * (WAVES * PER); r0 < a.tokens; r0 += (uint64_t)gridDim.x * (WAVES * PER)) {
-        const uint64_t r = r0 + mine, row = r < a.tokens ? r : a.tokens - 1;
+    const uint64_t step = (uint64_t)gridDim.x * ROWS;
+    struct Row {
         T t[V];
-        load_row<T, V>(logits + row * a.ld, a.experts, sub, vec, t);
-        float v[V], sum = 0.f;
-        softmax<T, LANES, V>(t, !a.mask || a.mask[row], a.experts, sub, v);
+        bool there;
+    } now, then;
+    auto load = [&](Row &to, uint64_t r) {
+        const uint64_t row = r < a.tokens ? r : a.tokens - 1;
+        Share<T, LANES, V>::load(logits + row * a.ld, a.experts, sub, vec, to.t);
+        to.there = !a.mask || a.mask[row];
+    };
+    uint64_t r0 = (uint64_t)blockIdx.x * ROWS;   // below the number of tokens
+    load(now, r0 + mine);
+    const uint32_t rows = (uint32_t)*a.rows;
+    const float dloss = a.dloss ? *a.dloss : 0.f;
+    // what the experts' probabilities are worth; the lanes of a row have all experts' counts
+    typedef Share<T, LANES, V> Mine;
+    int32_t c[V];
+    float g[V];
+    uint32_t picks = 0;
 #pragma unroll
-        for (int i = 0; i < V; i++) sum += g[i] * v[i];
-        sum = row_sum<LANES>(sum);
-#pragma unroll
-        for (int i = 0; i < V; i++) t[i] = Elem<T>::put(v[i] * (g[i] - sum));
-        if (r >= a.tokens) continue;
-        T *out = static_cast<T *>(a.dlogits) + row * a.ld_d;
-        const uint32_t e0 = sub * V;
-        if (vec && e0 + V <= a.experts) {
-            __builtin_memcpy(__builtin_assume_aligned(out + e0, sizeof t < 16 ? sizeof t : 16), t, sizeof t);
+    for (int i = 0; i < V; i += Mine::PIECE) {
+        const uint32_t e = Mine::expert(sub, i);
+        if (e + Mine::PIECE <= a.experts) {
+            __builtin_memcpy(c + i, a.counts + e, Mine::PIECE * 4);
+            if (a.dprobs) __builtin_memcpy(g + i, a.dprobs + e, Mine::PIECE * 4);
             continue;
         }
 #pragma unroll
-        for (int i = 0; i < V; i++)
-            if (e0 + i < a.experts) out[e0 + i] = t[i];
+        for (int j = 0; j < Mine::PIECE; j++) {
+            c[i + j] = e + j < a.experts ? a.counts[e + j] : 0;
+            g[i + j] = a.dprobs && e + j < a.experts ? a.dprobs[e + j] : 0.f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V; i++) picks += (uint32_t)c[i];
+    picks = reduce<LANES>(picks, [](uint32_t a, uint32_t b) { return a + b; });
+    const float each = rows ? 1.f / (float)rows : 0.f;
+    const float unit = picks ? dloss * ((float)a.experts / (float)picks) : 0.f;
+#pragma unroll
+    for (int i = 0; i < V; i++) g[i] = (unit * (float)c[i] + (a.dprobs ? g[i] : 0.f)) * each;
+    for (; r0 < a.tokens; r0 += step) {
+        if (r0 + step < a.tokens) load(then, r0 + step + mine);
+        float v[V], sum = 0.f;
+        softmax<T, LANES, V>(now.t, now.there, v);
+#pragma unroll
+        for (int i = 0; i < V; i++) sum += g[i] * v[i];
+        sum = row_sum<LANES>(sum);
+        T t[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) t[i] = Elem<T>::put(v[i] * (g[i] - sum));
+        now = then;
+        const uint64_t r = r0 + mine;
+        if (r >= a.tokens) continue;
+        Share<T, LANES, V>::store(static_cast<T *>(a.dlogits) + r * a.ld_d, a.experts, sub, vec, t);
     }
 }
 
-// A lane's neighbouring logits are read at once where every row starts on them.
-template <class T, int V>
+// A lane's pieces are read at once where every row starts on them.
+template <class T, int LANES, int V>
 bool whole(const void *p, uint64_t ld)
 {
-    const uint64_t unit = sizeof(T) * V < 16 ? sizeof(T) * V : 16;
-    return (reinterpret_cast<uintptr_t>(p) | (ld * sizeof(T))) % unit == 0;
+    return (reinterpret_cast<uintptr_t>(p) | (ld * sizeof(T))) % (Share<T, LANES, V>::PIECE * sizeof(T)) == 0;
 }
 
 inline uint32_t rows_at_a_time(uint32_t experts) { return WAVES * (experts <= NARROW_EXPERTS ? 4u : 1u); }
@@ -253,8 +390,11 @@ struct Forward {
     static hipError_t run(const BalanceArgs &a, hipStream_t s)
     {
         const uint32_t groups = workgroups(a.tokens, a.experts);
-        k_balance<T, LANES, V><<<dim3(groups), THREADS, 0, s>>>(a, whole<T, V>(a.logits, a.ld));
-        k_balance_join<<<dim3((a.experts + JOIN_EXPERTS - 1) / JOIN_EXPERTS), THREADS, 0, s>>>(a, groups);
+        k_balance<T, LANES, V><<<dim3(groups), THREADS, 0, s>>>(a, whole<T, LANES, V>(a.logits, a.ld));
+        uint32_t log = 0;
+        while ((1u << log) < a.experts) log++;
+        if (groups <= LOADS * (THREADS >> log)) k_balance_join<<<dim3(1), THREADS, 0, s>>>(a, groups, log);
+        else k_balance_join_many<<<dim3((a.experts + JOIN_EXPERTS - 1) / JOIN_EXPERTS), THREADS, 0, s>>>(a, groups);
         return hipGetLastError();
     }
 };
@@ -263,9 +403,9 @@ struct Backward {
     template <class T, int LANES, int V>
     static hipError_t run(const BalanceBackwardArgs &a, hipStream_t s)
     {
-        const bool vec = whole<T, V>(a.dlogits, a.ld_d) && whole<T, V>(a.logits, a.ld);
-        const uint64_t per = WAVES * 64 / LANES, n = (a.tokens + per - 1) / per;
-        k_balance_backward<T, LANES, V><<<dim3((uint32_t)(n < 2048 ? n : 2048)), THREADS, 0, s>>>(a, vec);
+        const bool vec = whole<T, LANES, V>(a.dlogits, a.ld_d) && whole<T, LANES, V>(a.logits, a.ld);
+        const uint64_t per = BACK_WAVES * 64 / LANES, n = (a.tokens + per - 1) / per;
+        k_balance_backward<T, LANES, V><<<dim3((uint32_t)(n < BACK_GROUPS ? n : BACK_GROUPS)), BACK_THREADS, 0, s>>>(a, vec);
         return hipGetLastError();
     }
 };

@@ -194,13 +194,14 @@ __device__ inline u32x2 codes8(const Eight<T> &o, uint32_t byte)
     return u32x2{codes4<T>(o.w, s), codes4<T>(o.w + Eight<T>::W / 2, s)};
 }
 
-// The rows alone: a wave packs 512 values of eight rows, so that what it reads,
+constexpr int ROWS = 2;   // of a wave
+
+// The rows alone: a wave packs 512 values of two rows, so that what it reads,
 // its codes and its scales are contiguous (1 KiB of 16-bit values, 512 and 4
 // bytes a row).  Bound by memory.
 template <class T>
 __global__ __launch_bounds__(256) void k_f8_rows(F8QuantizeArgs a, uint32_t chunks)
 {
-    constexpr int ROWS = 8;
     const T *x = static_cast<const T *>(a.x);
     const uint32_t lane = threadIdx.x & 63u;
     const uint64_t item = (uint64_t)blockIdx.x * 4u + (threadIdx.x >> 6);
@@ -234,9 +235,9 @@ constexpr uint32_t TILE = 128;   // rows and columns of a workgroup's tile: one 
 // rows, eight bytes at a time, and put together in LDS, from where whole columns
 // are stored: piece u (8 bytes) of column c stands at u ^ 2 (c / 8 % 8).
 // Bound by memory: every value is read once for both directions.
-//   ROWS: the rows' packing too.  TILES: one scale for the whole tile.
+//   BOTH: the rows' packing too.  TILES: one scale for the whole tile.
 // With `groups` the tile's rows are a block of one expert's.
-template <class T, bool ROWS, bool TILES>
+template <class T, bool BOTH, bool TILES>
 __global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_tiles, uint32_t row_tiles, uint32_t stored)
 {
     __shared__ __align__(16) uint8_t turned[TILE * TILE];
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_
 
     uint32_t rowtop[8];
 #pragma unroll
-    for (int p = 0; p < 8; p++) rowtop[p] = ROWS || TILES ? top_of(o[p]) : 0u;
+    for (int p = 0; p < 8; p++) rowtop[p] = BOTH || TILES ? top_of(o[p]) : 0u;
     uint32_t tile_byte = 0;
     if constexpr (TILES) {
         uint32_t t = 0;
@@ -273,7 +274,7 @@ __global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_
         for (int w = 0; w < 4; w++) t = tops[w][0] > t ? tops[w][0] : t;
         tile_byte = F8In<T>::byte(t);
     }
-    if constexpr (ROWS) {
+    if constexpr (BOTH) {
         const uint64_t cb = f8_code_bytes(a.cols), sb = f8_scale_bytes(a.cols);
 #pragma unroll
         for (int p = 0; p < 8; p++) {
@@ -384,14 +385,14 @@ hipError_t quantize_as(const F8QuantizeArgs &a, hipStream_t s)
 {
     if (!a.codes_t && !a.tiles) {   // one matrix
         const uint32_t chunks = (uint32_t)((a.cols + 511) / 512);
-        const uint64_t most = most_blocks(256) * 4 / chunks * 8;   // rows of a launch
+        const uint64_t most = most_blocks(256) * 4 / chunks * ROWS;   // rows of a launch
         for (uint64_t r = 0; r < a.rows; r += most) {
             F8QuantizeArgs part = a;
             part.x = static_cast<const T *>(a.x) + r * a.ld;
             part.rows = a.rows - r < most ? a.rows - r : most;
             part.codes += r * f8_code_bytes(a.cols);
             part.scales += r * f8_scale_bytes(a.cols);
-            const uint64_t items = (part.rows + 7) / 8 * chunks;
+            const uint64_t items = (part.rows + ROWS - 1) / ROWS * chunks;
             k_f8_rows<T><<<dim3((uint32_t)((items + 3) / 4)), 256, 0, s>>>(part, chunks);
         }
         return hipGetLastError();
@@ -417,7 +418,7 @@ __device__ inline void put8(T *p, const float v[8], bool vec, uint64_t left)
         u32x4 w[sizeof t / 16];
         __builtin_memcpy(w, t, sizeof t);
 #pragma unroll
-        for (unsigned i = 0; i < sizeof t / 16; i++) reinterpret_cast<u32x4 *>(p)[i] = w[i];
+        for (unsigned i = 0; i < sizeof t / 16; i++) __builtin_nontemporal_store(w[i], reinterpret_cast<u32x4 *>(p) + i);
         return;
     }
 #pragma unroll
