@@ -563,7 +563,8 @@ pccl_status pccl_moe_groups(pccl_ctx *ctx, const int32_t *counts, uint32_t exper
  * with largest magnitude a has the smallest scale, 2^-127 or more, with a <= 448
  * of it (so nothing is clipped); values go to the nearest, ties to the even code.
  * A block of zeros has b = 0; one that holds a NaN or an infinity b = 255: all
- * NaN.  With `tiles` (both pairs are needed) 128 x 128 values share a scale: rows
+ * NaN.  (What rounds to 2^128 is an infinity in any type that it is unpacked to.)
+ * With `tiles` (both pairs are needed) 128 x 128 values share a scale: rows
  * and columns stand for the same values, as the forward product and the input
  * gradient of a layer need of its weights.
  * Limit with columns or tiles: 2^24 - 1 tiles of 128 x 128 values.
@@ -656,7 +657,7 @@ pccl_status pccl_moe_balance(pccl_ctx *ctx, const void *logits, pccl_dtype dtype
  * stride ld_d), given pccl_moe_balance's counts and rows, dloss (one f32) and
  * dprobs[experts]; either may be NULL: that output has no gradient.  With counts
  * and rows that are sums over several ranks it is this rank's part of the
- * gradient of the loss of their joint batch.
+ * gradient of the loss of their joint batch.  Rows that do not count get zeros.
  */
 pccl_status pccl_moe_balance_backward(pccl_ctx *ctx, const void *logits, pccl_dtype dtype, uint64_t tokens,
                                       uint32_t experts, uint64_t ld, const uint8_t *token_mask,

@@ -357,13 +357,13 @@ __global__ __launch_bounds__(BACK_THREADS) void k_balance_backward(BalanceBackwa
     for (; r0 < a.tokens; r0 += step) {
         if (r0 + step < a.tokens) load(then, r0 + step + mine);
         float v[V], sum = 0.f;
-        softmax<T, LANES, V>(now.t, now.there, v);
+        const bool any = softmax<T, LANES, V>(now.t, now.there, v);
 #pragma unroll
         for (int i = 0; i < V; i++) sum += g[i] * v[i];
         sum = row_sum<LANES>(sum);
         T t[V];
 #pragma unroll
-        for (int i = 0; i < V; i++) t[i] = Elem<T>::put(v[i] * (g[i] - sum));
+        for (int i = 0; i < V; i++) t[i] = Elem<T>::put(any ? v[i] * (g[i] - sum) : 0.f);   // whatever dloss is
         now = then;
         const uint64_t r = r0 + mine;
         if (r >= a.tokens) continue;

@@ -396,28 +396,25 @@ class Operators:
         return F8(self._empty(torch.uint8, *shape[:-1], cb), self._empty(torch.uint8, *shape[:-1], sb), shape[-1])
 
     def _pack8(self, x, rows_too, cols_too, tiles=False, groups=None):
-        lead = ()
+        lead, batch = (), 1
         if tiles and x.dim() == 3:
-            lead = (x.shape[0],)
+            lead, batch = x.shape[:1], x.shape[0]
             try:
-                x = x.view(-1, x.shape[2])
+                x = x.view(batch * x.shape[1], x.shape[2])
             except RuntimeError:
                 raise ValueError(f"x: matrices that stand one behind the other are needed (strides {x.stride()})") from None
         rows, cols, ld = self._matrix("x", x)
-        batch = 1
-        if lead:
-            batch = lead[0]
-            rows = rows // batch if batch else 0
+        rows = rows // batch if batch else 0
+        if groups is not None and groups.rows != rows:
+            raise ValueError(f"x: {groups.rows} rows are grouped, got {rows}")
         r = c = rc = rs = cc = cs = None
         if rows_too:
             r = self._room8(*lead, rows, cols)
             rc, rs = r.codes.data_ptr(), r.scales.data_ptr()
         if cols_too:
-            c = self._room8(*lead, cols, 128 * group_blocks(groups.experts, rows) if groups else rows)
+            c = self._room8(*lead, cols, rows if groups is None else 128 * group_blocks(groups.experts, rows))
             cc, cs = c.codes.data_ptr(), c.scales.data_ptr()
         if groups is not None:
-            if groups.rows != rows:
-                raise ValueError(f"x: {groups.rows} rows are grouped, got {rows}")
             self._call(self._lib.pccl_f8_quantize_experts, x.data_ptr(), _DTYPE[x.dtype], rows, cols, ld, self._blocks(groups),
                        groups.experts, rc, rs, cc, cs, self._stream())
         else:
