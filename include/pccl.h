@@ -567,7 +567,7 @@ pccl_status pccl_moe_groups(pccl_ctx *ctx, const int32_t *counts, uint32_t exper
  * With `tiles` (both pairs are needed) 128 x 128 values share a scale: rows
  * and columns stand for the same values, as the forward product and the input
  * gradient of a layer need of its weights.
- * Limit with columns or tiles: 2^24 - 1 tiles of 128 x 128 values.
+ * Limit with columns or tiles: 2^23 - 1 tiles of 128 x 128 values.
  */
 pccl_status pccl_f8_quantize(pccl_ctx *ctx, const void *x, pccl_dtype dtype, uint64_t batch, uint64_t rows,
                              uint64_t cols, uint64_t ld, int tiles, uint8_t *codes, uint8_t *scales,
@@ -579,6 +579,7 @@ pccl_status pccl_f8_quantize(pccl_ctx *ctx, const void *x, pccl_dtype dtype, uin
  * PCCL_GROUP_BLOCKS(experts, rows) blocks, block j holding the rows of the j-th
  * one and zeros behind them.  What belongs to no expert is left as it was: rows
  * behind the last expert's, and blocks of the columns behind the last one's.
+ * Limit: 2^23 - 1 tiles of 128 columns of a block.
  */
 pccl_status pccl_f8_quantize_experts(pccl_ctx *ctx, const void *x, pccl_dtype dtype, uint64_t rows,
                                      uint64_t cols, uint64_t ld, const int32_t *groups, uint32_t experts,

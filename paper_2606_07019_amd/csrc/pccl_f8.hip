@@ -229,19 +229,22 @@ __global__ __launch_bounds__(256) void k_f8_rows(F8QuantizeArgs a, uint32_t chun
 
 constexpr uint32_t TILE = 128;   // rows and columns of a workgroup's tile: one block either way
 
-// One workgroup packs a tile of 128 x 128 values.  A lane holds eight values of
-// eight neighbouring rows; sixteen lanes share a row's block, and the largest of
-// the columns meet in LDS.  A column's codes are made in the lanes that hold its
-// rows, eight bytes at a time, and put together in LDS, from where whole columns
-// are stored: piece u (8 bytes) of column c stands at u ^ 2 (c / 8 % 8).
+// One workgroup packs a tile of 128 x 128 values.  A lane holds eight values of HELD
+// neighbouring rows; sixteen lanes share a row's block, and the largest of the
+// columns meet in LDS.  A column's codes are made in the lanes that hold its rows,
+// HELD bytes at a time, and put together in LDS, from where whole columns are
+// stored: piece u (8 bytes) of column c stands at u ^ 2 (c / 8 % 8).
 // Bound by memory: every value is read once for both directions.
 //   BOTH: the rows' packing too.  TILES: one scale for the whole tile.
 // With `groups` the tile's rows are a block of one expert's.
+// Eight waves a tile (2040 x 1500 of bf16 both ways 8.7 us; four, of eight rows a lane, 11.8).
+constexpr int HELD = 4, TILE_THREADS = 2048 / HELD, TILE_WAVES = TILE_THREADS / 64;
+
 template <class T, bool BOTH, bool TILES>
-__global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_tiles, uint32_t row_tiles, uint32_t stored)
+__global__ __launch_bounds__(TILE_THREADS) void k_f8_tile(F8QuantizeArgs a, uint32_t col_tiles, uint32_t row_tiles, uint32_t stored)
 {
     __shared__ __align__(16) uint8_t turned[TILE * TILE];
-    __shared__ uint32_t tops[4][TILE];
+    __shared__ __align__(16) uint32_t tops[TILE_WAVES][TILE];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const uint32_t tc = blockIdx.x % col_tiles, rest = blockIdx.x / col_tiles, tr = rest % row_tiles, matrix = rest / row_tiles;
     uint64_t first = (uint64_t)matrix * a.rows + (uint64_t)tr * TILE;
@@ -252,32 +255,32 @@ __global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_
         n = (uint32_t)entry[1] >> 16;
         if (n == 0) return;
     }
-    const uint32_t cg = lane & 15u, r0 = wave * 32u + (lane >> 4) * 8u;
+    const uint32_t cg = lane & 15u, r0 = (wave * 4u + (lane >> 4)) * HELD;
     const uint64_t col = (uint64_t)tc * TILE + cg * 8u;
     const T *x = static_cast<const T *>(a.x);
-    Eight<T> o[8];
+    Eight<T> o[HELD];
 #pragma unroll
-    for (int p = 0; p < 8; p++) o[p] = r0 + p < n && col < a.cols ? load8<T>(x + (first + r0 + p) * a.ld + col, a.cols - col) : nothing<T>();
+    for (int p = 0; p < HELD; p++) o[p] = r0 + p < n && col < a.cols ? load8<T>(x + (first + r0 + p) * a.ld + col, a.cols - col) : nothing<T>();
 
-    uint32_t rowtop[8];
+    uint32_t rowtop[HELD];
 #pragma unroll
-    for (int p = 0; p < 8; p++) rowtop[p] = BOTH || TILES ? top_of(o[p]) : 0u;
+    for (int p = 0; p < HELD; p++) rowtop[p] = BOTH || TILES ? top_of(o[p]) : 0u;
     uint32_t tile_byte = 0;
     if constexpr (TILES) {
         uint32_t t = 0;
 #pragma unroll
-        for (int p = 0; p < 8; p++) t = rowtop[p] > t ? rowtop[p] : t;
+        for (int p = 0; p < HELD; p++) t = rowtop[p] > t ? rowtop[p] : t;
         t = row_max<64>(t);
         if (lane == 0) tops[wave][0] = t;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < 4; w++) t = tops[w][0] > t ? tops[w][0] : t;
+        for (int w = 0; w < TILE_WAVES; w++) t = tops[w][0] > t ? tops[w][0] : t;
         tile_byte = F8In<T>::byte(t);
     }
     if constexpr (BOTH) {
         const uint64_t cb = f8_code_bytes(a.cols), sb = f8_scale_bytes(a.cols);
 #pragma unroll
-        for (int p = 0; p < 8; p++) {
+        for (int p = 0; p < HELD; p++) {
             const uint32_t byte = TILES ? tile_byte : F8In<T>::byte(row_max<16>(rowtop[p]));
             const u32x2 code = codes8(o[p], byte);
             if (r0 + p < n) {
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_
             for (int i = 0; i < 8; i++) {
                 top[i] = 0;
 #pragma unroll
-                for (int p = 0; p < 8; p++) {
+                for (int p = 0; p < HELD; p++) {
                     const uint32_t v = o[p].w[i] & 0x7FFFFFFFu;
                     top[i] = v > top[i] ? v : top[i];
                 }
@@ -318,7 +321,7 @@ __global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_
             for (int i = 0; i < 4; i++) {
                 u16x2 t = {0, 0};
 #pragma unroll
-                for (int p = 0; p < 8; p++) t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, o[p].w[i] & 0x7FFF7FFFu));
+                for (int p = 0; p < HELD; p++) t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, o[p].w[i] & 0x7FFF7FFFu));
 #pragma unroll
                 for (int x = 16; x < 64; x <<= 1)
                     t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, __shfl_xor(__builtin_bit_cast(int, t), x)));
@@ -334,7 +337,7 @@ __global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_
 #pragma unroll
         for (int i = 0; i < 8; i++) top[i] = 0;
 #pragma unroll
-        for (int w = 0; w < 4; w++)
+        for (int w = 0; w < TILE_WAVES; w++)
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 const u32x4 t = *reinterpret_cast<const u32x4 *>(&tops[w][cg * 8 + h * 4]);
@@ -344,18 +347,21 @@ __global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_
 #pragma unroll
         for (int i = 0; i < 8; i++) bytes[i] = F8In<T>::byte(top[i]);
     }
-    const uint32_t unit = ((wave * 4u + (lane >> 4)) ^ ((cg & 7u) * 2u)) * 8u;
+    const uint32_t unit = ((r0 / 8u) ^ ((cg & 7u) * 2u)) * 8u + r0 % 8u;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        Eight<T> v;   // the column's eight rows
+        uint32_t v[HELD * sizeof(T) / 4];   // the column's rows
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int p = 0; p < 8; p++) v.w[p] = o[p].w[i];
+            for (int p = 0; p < HELD; p++) v[p] = o[p].w[i];
         } else {
 #pragma unroll
-            for (int p = 0; p < 4; p++) v.w[p] = __builtin_amdgcn_perm(o[2 * p + 1].w[i / 2], o[2 * p].w[i / 2], i % 2 ? 0x07060302u : 0x05040100u);
+            for (int p = 0; p < HELD / 2; p++) v[p] = __builtin_amdgcn_perm(o[2 * p + 1].w[i / 2], o[2 * p].w[i / 2], i % 2 ? 0x07060302u : 0x05040100u);
         }
-        *reinterpret_cast<u32x2 *>(turned + (cg * 8u + i) * TILE + unit) = codes8(v, bytes[i]);
+        const float scale = mx_scale(bytes[i]);
+#pragma unroll
+        for (int p = 0; p < HELD / 4; p++)
+            *reinterpret_cast<uint32_t *>(turned + (cg * 8u + i) * TILE + unit + 4 * p) = bytes[i] == 255u ? 0u : codes4<T>(v + p * sizeof(T), scale);
     }
     // `stored`: blocks of a column that there is room for
     const uint64_t cbt = (uint64_t)stored * TILE, sbt = (stored + 3u) / 4u * 4u;
@@ -371,8 +377,8 @@ __global__ __launch_bounds__(256) void k_f8_tile(F8QuantizeArgs a, uint32_t col_
     }
     __syncthreads();
 #pragma unroll
-    for (uint32_t i = 0; i < 4; i++) {
-        const uint32_t c = i * 32u + threadIdx.x / 8, q = threadIdx.x % 8;   // 16 bytes of a column
+    for (uint32_t i = 0; i < 1024 / TILE_THREADS; i++) {
+        const uint32_t c = i * (TILE_THREADS / 8) + threadIdx.x / 8, q = threadIdx.x % 8;   // 16 bytes of a column
         const uint64_t cc = (uint64_t)tc * TILE + c;
         if (cc < a.cols)
             *reinterpret_cast<u32x4 *>(a.codes_t + (column0 + cc) * cbt + (uint64_t)tr * TILE + q * 16u) =
@@ -400,9 +406,9 @@ hipError_t quantize_as(const F8QuantizeArgs &a, hipStream_t s)
     const uint32_t ct = (uint32_t)f8_blocks(a.cols);
     const uint32_t rt = (uint32_t)(a.groups ? groups_blocks(a.experts, a.rows, 128) : f8_blocks(a.rows));
     const dim3 grid((uint32_t)(ct * (uint64_t)rt * a.batch));
-    if (a.tiles) k_f8_tile<T, true, true><<<grid, 256, 0, s>>>(a, ct, rt, rt);
-    else if (a.codes) k_f8_tile<T, true, false><<<grid, 256, 0, s>>>(a, ct, rt, rt);
-    else k_f8_tile<T, false, false><<<grid, 256, 0, s>>>(a, ct, rt, rt);
+    if (a.tiles) k_f8_tile<T, true, true><<<grid, TILE_THREADS, 0, s>>>(a, ct, rt, rt);
+    else if (a.codes) k_f8_tile<T, true, false><<<grid, TILE_THREADS, 0, s>>>(a, ct, rt, rt);
+    else k_f8_tile<T, false, false><<<grid, TILE_THREADS, 0, s>>>(a, ct, rt, rt);
     return hipGetLastError();
 }
 

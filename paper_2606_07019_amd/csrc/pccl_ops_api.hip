@@ -353,7 +353,7 @@ pccl_status pccl_f8_quantize(pccl_ctx *c, const void *x, pccl_dtype dtype, uint6
         NEED(codes || scales || codes_t || scales_t, "no output");
         if (codes || scales || tiles) TRY(check_packed(c, "rows", codes, scales));
         if (codes_t || scales_t || tiles) TRY(check_packed(c, "columns", codes_t, scales_t));
-        LIMIT(!codes_t || f8_blocks(rows) * f8_blocks(cols) <= most_blocks(256) / batch, "%llu x %llu x %llu (limit 2^24 - 1 tiles of 128 x 128)",
+        LIMIT(!codes_t || f8_blocks(rows) * f8_blocks(cols) <= most_blocks(512) / batch, "%llu x %llu x %llu (limit 2^23 - 1 tiles of 128 x 128)",
               (ull)batch, (ull)rows, (ull)cols);
         LIMIT(!codes_t || batch * cols <= OPS_MAX_EXTENT, "%llu columns of %llu matrices (limit 2^31 - 1)", (ull)cols, (ull)batch);
         OnDevice device;
@@ -376,7 +376,7 @@ pccl_status pccl_f8_quantize_experts(pccl_ctx *c, const void *x, pccl_dtype dtyp
         NEED(groups && aligned(groups, 4), "groups are null or misaligned");
         if (codes || scales) TRY(check_packed(c, "rows", codes, scales));
         TRY(check_packed(c, "columns", codes_t, scales_t));
-        TRY(check_grid(c, groups_blocks(experts, rows, 128) * f8_blocks(cols), 256));
+        TRY(check_grid(c, groups_blocks(experts, rows, 128) * f8_blocks(cols), 512));
         OnDevice device;
         TRY(device.enter(c));
         const F8QuantizeArgs a{x, 1, rows, cols, ld, codes, scales, codes_t, scales_t, 0, experts, groups};

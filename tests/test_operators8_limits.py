@@ -66,14 +66,14 @@ assert attempt(W, None, None, None, None, 0, 2, 4, 4, M, M, 0) == 1      # no ro
 B = P.pccl_moe_balance
 space = P.pccl_moe_balance_workspace(h, 100, 8)
 ok = (M, 0, 100, 8, 8, M, 2, None, M, M, M, M)
-assert attempt(B, *ok, M, space) == 2
+assert attempt(B, *ok, M, space) == 1 and attempt(B, M, 0, 1000, 8, 8, M, 2, None, M, M, M, M, M, 1 << 30) == 2
 assert attempt(B, *ok, M, space - 1) == EM and attempt(B, *ok) == EI and attempt(B, *ok, M + 4, space) == EI
 for i, bad, want in ((1, 9, EI), (3, 0, EI), (3, 1025, EU), (4, 7, EI), (5, None, EI), (6, 0, EI), (6, 9, EI), (8, None, EI), (9, None, EI), (10, None, EI), (11, M + 2, EI)):
     args = list(ok)
     args[i] = bad
     assert attempt(B, *args, M, space) == want, (i, bad)
 assert attempt(B, M, 0, 100, 1025, 1025, M, 2, None, M, M, M, M, M, 1 << 30) == EU
-assert attempt(B, None, 0, 0, 8, 8, None, 2, None, M, M, M, M, M, space) == 2   # no tokens: zeros
+assert attempt(B, None, 0, 0, 8, 8, None, 2, None, M, M, M, M, M, space) == 1   # no tokens: zeros
 K = P.pccl_moe_balance_backward
 assert attempt(K, M, 0, 4, 8, 8, None, M, M, M, None, M, 8) == 1 and attempt(K, M, 0, 4, 8, 8, None, M, M, None, None, M, 8) == 1
 assert attempt(K, M, 0, 4, 8, 8, None, None, M, M, None, M, 8) == EI and attempt(K, M, 0, 4, 8, 8, None, M, None, M, None, M, 8) == EI
@@ -98,10 +98,10 @@ for rows, cols in ((1000, 70000), (1 << 26, 8), (TOP, 1), (1 << 24, 70000)):
         assert start == at and n > 0
         at += n * ((cols + 127) // 128 * 128)
     assert at == M + rows * ((cols + 127) // 128 * 128), (rows, cols)
-for batch, rows, cols, want in ((1, 70000, 70000, 1), (1, 128, TOP, EU), (1, 128, TOP - 128, 1), (1, TOP, 128, EU), (61, 1000, 2040, 1), (1 << 12, 1 << 12, 1 << 12, 1), (1 << 13, 1 << 13, 1 << 13, EU)):
+for batch, rows, cols, want in ((1, 70000, 70000, 1), (1, 256, TOP, EU), (1, 128, (1 << 30) - 128, 1), (1, TOP, 128, EU), (61, 1000, 2040, 1), (1 << 12, 1 << 12, 1 << 12, 1), (1 << 13, 1 << 13, 1 << 13, EU)):
     for tiles in (0, 1):
         assert attempt(P.pccl_f8_quantize, M, P.PCCL_BF16, batch, rows, cols, cols, tiles, M, M, M, M) == want, (batch, rows, cols)
-for rows, cols, want in ((1 << 20, 8192, 1), (TOP, 128, EU), (TOP - 2000 * 128, 1, 1)):
+for rows, cols, want in ((1 << 20, 8192, 1), (1 << 30, 128, EU), ((1 << 30) - 2000 * 128, 1, 1)):
     assert attempt(P.pccl_f8_quantize_experts, M, P.PCCL_BF16, rows, cols, cols, M, 1000, M, M, M, M) == want, (rows, cols)
 for m, n, k, want in ((131072, 131072, 256, 1), (200000, 200000, 256, 1), (1, 1 << 27, 256, 1), (64, TOP, 256, 1), (1 << 20, 1 << 20, 256, EU),
                       (TOP, 1, 256, EU), (65, TOP, 256, EU), (70, 10000, 1 << 23, 2), (70, 20000, 1 << 23, 1), (1, 100, 1 << 23, 2), (64, TOP, 1 << 14, EU)):
@@ -112,7 +112,7 @@ for rows, experts, m, n, want in ((1 << 20, 1024, 8192, 8192, 1), (1 << 20, 1024
     assert attempt(P.pccl_f8_expert_gradient, M, M, M, M, rows, experts, m, n, M, M, P.PCCL_F32) == want, (rows, experts, m, n)
 for experts, rows in ((1024, TOP), (1, 0), (1024, 5)):
     assert attempt(P.pccl_moe_groups, M, experts, rows, M) == 1
-for tokens, experts, topk, want in ((TOP // 8, 8, 8, 2), (TOP // 32, 1024, 32, 2), (TOP // 8 + 1, 8, 8, EU), (0, 300, 3, 2)):
+for tokens, experts, topk, want in ((TOP // 8, 8, 8, 2), (TOP // 32, 1024, 32, 2), (TOP // 8 + 1, 8, 8, EU), (0, 300, 3, 1)):
     assert attempt(P.pccl_moe_balance, M, P.PCCL_F32, tokens, experts, experts, M, topk, None, M, M, M, M, M, 1 << 40) == want, (tokens, experts)
 for tokens, experts in ((TOP, 1), (TOP, 1024), (1, 300)):
     assert attempt(P.pccl_moe_balance_backward, M, P.PCCL_F32, tokens, experts, experts, None, M, M, M, M, M, experts) == 1
