@@ -35,7 +35,8 @@ __device__ inline uint64_t scan64(uint64_t v, uint64_t *sums)
 }
 
 // Every workgroup sums up the counts (a negative one is none, rows past `rows`
-// are no one's) and fills its share of the two lists, a block a thread.
+// are no one's) and fills its share of the two lists, a block a thread.  Bound by
+// its launch and two scans: 64 experts, 512 rows, 4.6 us; 32,768 rows 6.0.
 __global__ __launch_bounds__(GROUP_THREADS) void k_groups(GroupsArgs a)
 {
     __shared__ uint32_t first[ROUTE_MAX_EXPERTS + 1], start[2][ROUTE_MAX_EXPERTS + 1];
@@ -198,7 +199,8 @@ constexpr int ROWS = 2;   // of a wave
 
 // The rows alone: a wave packs 512 values of two rows, so that what it reads,
 // its codes and its scales are contiguous (1 KiB of 16-bit values, 512 and 4
-// bytes a row).  Bound by memory.
+// bytes a row).  Bound by memory: 8192 x 8192 of bf16 32 us, 6.3 TB/s from and to the
+// device's cache.
 template <class T>
 __global__ __launch_bounds__(256) void k_f8_rows(F8QuantizeArgs a, uint32_t chunks)
 {
@@ -234,7 +236,8 @@ constexpr uint32_t TILE = 128;   // rows and columns of a workgroup's tile: one 
 // columns meet in LDS.  A column's codes are made in the lanes that hold its rows,
 // HELD bytes at a time, and put together in LDS, from where whole columns are
 // stored: piece u (8 bytes) of column c stands at u ^ 2 (c / 8 % 8).
-// Bound by memory: every value is read once for both directions.
+// Bound by memory: every value is read once for both directions (16384 x 4096 of
+// bf16 both ways 46 us, 5.8 TB/s; 61 matrices of 1000 x 2040 in tiles 99 us, 5 TB/s).
 //   BOTH: the rows' packing too.  TILES: one scale for the whole tile.
 // With `groups` the tile's rows are a block of one expert's.
 // Eight waves a tile (2040 x 1500 of bf16 both ways 8.7 us; four, of eight rows a lane, 11.8).
@@ -432,7 +435,9 @@ __device__ inline void put8(T *p, const float v[8], bool vec, uint64_t left)
         if ((uint64_t)i < left) p[i] = t[i];
 }
 
-// A wave unpacks 512 values of a row, eight a lane.  Bound by writing them.
+// A wave unpacks 512 values of a row, eight a lane.  Bound by writing them: 16384 x
+// 4096 of bf16 31 us, 6.4 TB/s read and written (stored through the caches a pass of
+// packing both ways and unpacking both took 137 us, so 113).
 template <class T>
 __global__ __launch_bounds__(256) void k_f8_unpack(F8DequantizeArgs a, uint32_t chunks, bool vec)
 {

@@ -168,6 +168,18 @@ __device__ inline void deal(uint32_t id, uint32_t mt, uint32_t nt, uint32_t &m, 
 // a whole stage's time.  In LDS chunk c (16 bytes) of row r stands at chunk c ^ (r
 // / 2 % 8) of the row, so the 16 lanes that read one chunk of 16 rows meet every
 // bank once.
+// 8192^3 takes 391 us, 2.8 PFLOP/s: the matrix units are busy 74 % of the cycles
+// (the instruction alone reaches 4.0), the rest are meetings and 12 us a tile of
+// first copies and stores.  With results of 32 bits 770 us, 1.4 PFLOP/s, bound by
+// the matrix units' 16-bit rate.  EXPERTS: bound by reading the weights where an
+// expert has few rows (512 rows of 64 experts, 2048 x 2048, 41 us, 6.5 TB/s), by the
+// products where it has many (32,768 rows, 4096 x 2048, 359 us, 1.5 PFLOP/s: one
+// expert's last block is half empty).  GRADIENT: bound by storing (61 experts, 1000 x
+// 2040 of f32, from 12,297 rows, 146 us, 3.4 TB/s), each tile's few stages before it
+// (without the stores 105).
+// A workgroup that goes through several tiles, the next one's first copies
+// under way while it stores, took longer everywhere (8192^3 425 us, that gradient 219):
+// a wait for copies is one for the stores before them.
 template <class T, bool EXACT, Kind KIND, int BM, int BN, int WM, int WN, int BUFFERS>
 __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uint32_t mt, uint32_t nt, uint32_t per)
 {
@@ -353,9 +365,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy outlives the workgroup's LDS
     }
     // The sums go through LDS, 32 rows of the wave's at a time, so that whole rows
-    // of them are stored, past the caches that the operands are read from (8192^3
-    // 445 us with ordinary stores, 433 with these; the gradient of 61 experts, 1000 x
-    // 2040 of f32, 243 and 167).
+    // of them are stored, past the caches that the operands are read from (with
+    // ordinary stores 8192^3 takes 3 % longer, the gradient of 61 experts, 1000 x 2040 of
+    // f32, 46 %).  Few instructions a chunk, as a wave has a SIMD to itself (checks of
+    // every chunk's columns cost that gradient 5 %).  Rows of it that begin inside a
+    // line of 128 bytes cost 20 %; their first and last lines kept in the caches, more.
     typedef u32x4 Chunk __attribute__((aligned(2)));   // at any address
     T *out = static_cast<T *>(a.out) + (KIND == EXPERTS ? 0u : (uint64_t)job.slice * a.m * a.ld);
     constexpr uint32_t COLS = BN / WN, EACH = 16 / sizeof(T), CHUNKS_ROW = COLS / EACH, ROW = COLS * sizeof(T) + 16;
@@ -373,23 +387,26 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
                 for (int c = 0; c < 4; c++) t[c] = Elem<T>::put(acc[i][j][4 * q + c]);
                 __builtin_memcpy(__builtin_assume_aligned(own + r * ROW + (j * 32u + q * 8u + half * 4u) * sizeof(T), sizeof t), t, sizeof t);
             }
+        constexpr uint32_t PASSES = CHUNKS_ROW / 2, EACH_PASS = 64 / CHUNKS_ROW;   // rows of a pass
+        const uint32_t row = lane / CHUNKS_ROW, n = wn + lane % CHUNKS_ROW * EACH;
+        Chunk w[PASSES];
 #pragma unroll
-        for (uint32_t p = 0; p < CHUNKS_ROW / 2; p++) {
-            const uint32_t row = p * (64u / CHUNKS_ROW) + lane / CHUNKS_ROW, col = lane % CHUNKS_ROW * EACH;
-            const uint32_t m = wm + i * 32u + row, n = wn + col;
-            if (m >= job.rows_a || n >= job.rows_b) continue;
-            T t[EACH];
-            __builtin_memcpy(t, __builtin_assume_aligned(own + row * ROW + col * sizeof(T), 16), 16);
-            T *to = out + (job.row + m) * a.ld + job.col + n;
-            if (n + EACH <= job.rows_b) {
-                Chunk w;
-                __builtin_memcpy(&w, t, 16);
-                __builtin_nontemporal_store(w, reinterpret_cast<Chunk *>(to));
-                continue;
+        for (uint32_t p = 0; p < PASSES; p++) w[p] = *reinterpret_cast<const u32x4 *>(own + (p * EACH_PASS + row) * ROW + lane % CHUNKS_ROW * 16u);
+        const uint32_t m = wm + i * 32u + row, left = m < job.rows_a ? job.rows_a - m : 0u;
+        T *to = out + (job.row + m) * a.ld + job.col + n;
+        if (n + EACH <= job.rows_b) {
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES; p++, to += EACH_PASS * a.ld)
+                if (p * EACH_PASS < left) __builtin_nontemporal_store(w[p], reinterpret_cast<Chunk *>(to));
+        } else if (n < job.rows_b) {   // a row's last few
+#pragma unroll
+            for (uint32_t p = 0; p < PASSES; p++, to += EACH_PASS * a.ld) {
+                T t[EACH];
+                __builtin_memcpy(t, &w[p], 16);
+#pragma unroll
+                for (uint32_t c = 0; c + 1 < EACH; c++)
+                    if (p * EACH_PASS < left && n + c < job.rows_b) to[c] = t[c];
             }
-#pragma unroll
-            for (uint32_t c = 0; c < EACH; c++)
-                if (n + c < job.rows_b) to[c] = t[c];
         }
     }
 }
@@ -434,7 +451,8 @@ constexpr uint32_t few_lds() { return WAVES * D * SLOT + 2 * WAVES * MT * 1024; 
 // operands come straight to LDS in whole pieces of 128 bytes a row, D steps ahead
 // in a ring of its own, so that nothing is between the waves but the joining of
 // their sums, in their order.  Whoever has no more to read reads one piece, so
-// that as many copies are under way.
+// that as many copies are under way.  48 x 16384 x 5120 takes 22.5 us from memory, 3.7
+// TB/s (the tiles' form 26.6), 16.9 from the device's cache; 1 x 4096 x 4096 6.3 (14.3).
 template <bool EXACT, int MT, int S, int WAVES, int D>
 __global__ __launch_bounds__(64 * WAVES) void k_f8_few(F8MatmulArgs a, uint32_t dtype, bool vec, uint32_t tiles)
 {
@@ -587,21 +605,28 @@ inline uint64_t tiles_of(uint64_t m, uint64_t n, uint64_t side = 128) { return (
 
 // Tiles of 256 x 256 or of 128 x 128, by rounds over 256 compute units.  A round
 // of the larger ones takes as long as three of the smaller ones (with k = 2048, in
-// us, large and small: 128 and 512 tiles 28 and 23, 160 and 640 28 and 31, 256 and
-// 1024 34 and 44, 272 and 1088 53 and 52, 384 and 1536 58 and 64), or, with
-// results of 32 bits, as three and a half (47 and 36, 47 and 46, 63 and 67, 100
-// and 77, 103 and 98).
+// us, large and small: 128 and 512 tiles 28 and 22, 160 and 640 28 and 30, 256 and
+// 1024 33 and 43, 272 and 1088 53 and 50, 384 and 1536 56 and 63), or, with results
+// of 32 bits, not quite as four (160 and 640 47 and 44, 256 and 1024 60 and 66, 272
+// and 1088 100 and 73, 384 and 1536 101 and 101; 32,768 rows of 64 experts, 4096 x
+// 2048, 603 and 575).
 inline bool large_tiles(uint64_t small, uint64_t large, bool exact)
 {
     const uint64_t s = (small + 255) / 256, l = (large + 255) / 256;
-    return exact ? 2 * s >= 7 * l : s >= 3 * l;
+    return exact ? 4 * s >= 15 * l : s >= 3 * l;
 }
 
 // How a product is made: k in `parts` of `per` blocks; few rows with steps of
 // `each` a wave.
+// As few rows, or in tiles, in us: 1 x 4096 x 4096 6.3 and 14.3, 64 x 4096 x 4096
+// 10.2 and 15.9, 64 x 16384 x 1024 8.9 and 9.2, 64 x 65536 x 2048 35.8 and 35.7.  More
+// rows than 64 leave no registers for them.
 constexpr uint32_t FEW_ROWS = 64;
 constexpr int FEW_WAVES = 8, FEW_AHEAD = 4;   // seven steps ahead take as long as four
-constexpr uint32_t LEAST_BLOCKS = 16;
+// Of a part of k in tiles.  With 4, 8 and 16, in us: 512 x 512 x 8192 20.3, 17.6 and
+// 19.3, 100 x 4096 x 4096 18.8, 15.6 and 17.5, with results of 32 bits 20.4, 17.5 and
+// 20.9; 500 x 1000 x 2048 12.8, 12.1 and 11.9.
+constexpr uint32_t LEAST_BLOCKS = 8;
 struct Plan {
     bool few;
     uint32_t parts, per, each;
@@ -621,7 +646,7 @@ inline Plan plan(uint64_t m, uint64_t n, uint64_t k)
         return p;
     }
     // Blocks of k that a workgroup takes: all, or, where tiles are too few for 256
-    // compute units, parts of sixteen blocks (2048 values) or more.
+    // compute units, parts of LEAST_BLOCKS or more.
     const uint64_t tiles = tiles_of(m, n), want = tiles < 256 ? 256 / tiles : 1;
     uint64_t per = (blocks + want - 1) / want;
     if (per < LEAST_BLOCKS) per = LEAST_BLOCKS;
@@ -652,7 +677,7 @@ hipError_t few_as(const F8MatmulArgs &a, uint32_t dtype, uint32_t slices, uint32
 template <bool EXACT, int MT>
 hipError_t few_rows(const F8MatmulArgs &a, uint32_t dtype, const Plan &p, hipStream_t s)
 {
-    const uint32_t workers = (256 + p.parts - 1) / p.parts;   // one a compute unit
+    const uint32_t workers = (256 + p.parts - 1) / p.parts;   // one a compute unit (two: 64 x 16384 x 1024 11.1 us for 8.9, 48 x 16384 x 5120 26.7 for 22.5)
 #define STEPS(S)                                                                                             \
     if constexpr (MT * S <= 16)                                                                              \
         if (p.each <= S) return few_as<EXACT, MT, S, FEW_WAVES, FEW_AHEAD>(a, dtype, p.parts, workers, s);
@@ -709,7 +734,7 @@ hipError_t launch_f8_matmul(const F8MatmulArgs &a, uint32_t dtype, hipStream_t s
             e = product<float, EXACT, DENSE, 128, 128, 2, 2, 4>(part, mt, p.parts, p.per, s);
         } else if (large_tiles(tiles_of(a.m, a.n), tiles_of(a.m, a.n, 256), EXACT)) {
             e = product<T, EXACT, DENSE, 256, 256, 2, 2, 2>(a, (mt + 1) / 2, 1, p.per, s);
-        } else if (tiles_of(a.m, a.n) > 256) {   // two workgroups a compute unit, with half as much copied ahead (2048^2 x 8192, one tile each, 44 and 50 us; 2080 x 2040 x 1500, 272 tiles, 20 and 15)
+        } else if (tiles_of(a.m, a.n) > 256) {   // two workgroups a compute unit, with half as much copied ahead (2048^2 x 8192, one tile each, 49 us and 44 without; 2040 x 2080 x 1500, 272 tiles, 15 and 19)
             e = product<T, EXACT, DENSE, 128, 128, 2, 2, 2>(a, mt, 1, p.per, s);
         } else {
             e = product<T, EXACT, DENSE, 128, 128, 2, 2, 4>(a, mt, 1, p.per, s);
@@ -723,7 +748,9 @@ hipError_t launch_f8_expert_matmul(const F8MatmulArgs &a, uint32_t dtype, hipStr
     return by_type(dtype, [&](auto t) -> hipError_t {
         typedef decltype(t) T;
         constexpr bool EXACT = sizeof(T) == 4;
-        // an expert's last block is half full, as far as one can know here
+        // an expert's last block is half full, as far as one can know here (large and
+        // small: 32,768 rows of 64 experts, 4096 x 2048, 359 and 394 us; 512 rows, 2048 x
+        // 2048, 55 and 42)
         const uint64_t half = a.experts / 2, small = (a.rows / 128 + half) * ((a.n + 127) / 128), large = (a.rows / 256 + half) * ((a.n + 255) / 256);
         if (large_tiles(small, large, EXACT))
             return product<T, EXACT, EXPERTS, 256, 256, 2, 2, 2>(a, (uint32_t)groups_blocks(a.experts, a.rows, 256), 1, 0, s);
@@ -736,6 +763,7 @@ hipError_t launch_f8_expert_gradient(const F8MatmulArgs &a, uint32_t dtype, hipS
     return by_type(dtype, [&](auto t) -> hipError_t {
         typedef decltype(t) T;
         constexpr bool EXACT = sizeof(T) == 4;
+        // large and small: 61 experts, 1000 x 2040 of f32, 151 and 161 us, of bf16 101 and 117
         if (large_tiles(a.experts * tiles_of(a.m, a.n), a.experts * tiles_of(a.m, a.n, 256), EXACT))
             return product<T, EXACT, GRADIENT, 256, 256, 2, 2, 2>(a, (uint32_t)((a.m + 255) / 256), a.experts, 0, s);
         return product<T, EXACT, GRADIENT, 128, 128, 2, 2, 2>(a, (uint32_t)((a.m + 127) / 128), a.experts, 0, s);

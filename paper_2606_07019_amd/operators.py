@@ -396,15 +396,15 @@ class Operators:
         return F8(self._empty(torch.uint8, *shape[:-1], cb), self._empty(torch.uint8, *shape[:-1], sb), shape[-1])
 
     def _pack8(self, x, rows_too, cols_too, tiles=False, groups=None):
-        lead, batch = (), 1
+        lead, batch, one = (), 1, None
         if tiles and x.dim() == 3:
-            lead, batch = x.shape[:1], x.shape[0]
+            lead, batch, one = x.shape[:1], x.shape[0], x.shape[1]
             try:
-                x = x.view(batch * x.shape[1], x.shape[2])
+                x = x.view(batch * one, x.shape[2])
             except RuntimeError:
                 raise ValueError(f"x: matrices that stand one behind the other are needed (strides {x.stride()})") from None
         rows, cols, ld = self._matrix("x", x)
-        rows = rows // batch if batch else 0
+        rows = rows if one is None else one
         if groups is not None and groups.rows != rows:
             raise ValueError(f"x: {groups.rows} rows are grouped, got {rows}")
         r = c = rc = rs = cc = cs = None

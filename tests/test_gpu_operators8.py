@@ -107,6 +107,11 @@ def test_packing_of_several_matrices(ops):
     for i in range(3):
         for q, one in zip((r, c), ops.quantize8_tiles(x[i])):
             assert t.equal(q.codes[i], one.codes) and t.equal(q.scales[i], one.scales)
+    for shape in ((0, 200, 140), (3, 0, 140), (3, 200, 0)):   # of none, and of matrices of nothing
+        for q, (rows, cols) in zip(ops.quantize8_tiles(x.new_empty(shape)), (shape[1:], shape[:0:-1])):
+            cb, sb = -(-cols // 128) * 128, -(-cols // 512) * 4
+            assert q.codes.shape == (shape[0], rows, cb) and q.scales.shape == (shape[0], rows, sb) and q.cols == cols
+            assert ops.dequantize8(q, t.float16).shape == (shape[0], rows, cols)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
