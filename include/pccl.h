@@ -633,7 +633,7 @@ pccl_status pccl_f8_expert_gradient(pccl_ctx *ctx, const uint8_t *a_codes, const
                                     uint32_t experts, uint64_t m, uint64_t n, const int32_t *groups,
                                     void *out, pccl_dtype dtype, void *hip_stream);
 
-/* Workspace of pccl_moe_balance. */
+/* Workspace of pccl_moe_balance; 0 where it needs none. */
 pccl_status pccl_moe_balance_workspace(pccl_ctx *ctx, uint64_t tokens, uint32_t experts, size_t *out_bytes);
 
 /*

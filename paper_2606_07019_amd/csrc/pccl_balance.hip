@@ -137,7 +137,7 @@ __global__ __launch_bounds__(THREADS) void k_balance(BalanceArgs a, bool vec)
     for (uint32_t e = threadIdx.x; e < LANES * V; e += THREADS) hist[e] = 0;
     __syncthreads();
     const Space s = space_of(a.ws, gridDim.x, a.experts);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *s.done = 0;   // for the joining kernel
+    if (gridDim.x > 1 && blockIdx.x == 0 && threadIdx.x == 0) *s.done = 0;   // for the joining kernel
     float acc[V];
 #pragma unroll
     for (int i = 0; i < V; i++) acc[i] = 0.f;
@@ -466,6 +466,7 @@ hipError_t by_type(const A &a, uint32_t dtype, hipStream_t s)
 size_t balance_workspace(uint64_t tokens, uint32_t experts)
 {
     const uint64_t groups = workgroups(tokens, experts);
+    if (groups == 1) return 0;
     return (size_t)((512 + 4 * groups * (1 + 2 * (uint64_t)experts) + 255) & ~255ull);
 }
 

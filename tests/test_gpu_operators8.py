@@ -389,6 +389,39 @@ def test_balance(ops, tokens, experts, topk, dtype, barred):
     t = _torch()
     rng = np.random.default_rng(tokens + experts)
     logits, ids, mask = _balance_inputs(rng, tokens, experts, topk, dtype, barred)
+    _balance_checked(ops, rng, logits, ids, mask, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,experts,topk", [(70, 61, 3), (300, 256, 8), (140, 520, 4)])
+def test_balance_of_lowest_values_of_padding_and_of_strided_rows(ops, tokens, experts, topk, dtype):
+    print(f"[operators8] balance {tokens}x{experts} lowest, padding, strides {dtype}", flush=True)
+    t = _torch()
+    rng = np.random.default_rng(tokens)
+    logits, ids, mask = _balance_inputs(rng, tokens, experts, topk, dtype, True)
+    lowest = t.finfo(logits.dtype).min
+    low = t.where(logits == -float("inf"), lowest, logits)        # barred by the type's lowest value: whole rows are even then
+    _balance_checked(ops, rng, low, ids, mask, dtype)
+    garbage = logits.clone()                                      # what padding holds does not count
+    off = (mask == 0).nonzero().flatten()
+    assert len(off) >= 3
+    garbage[off[0]], garbage[off[1]], garbage[off[2], 0] = float("nan"), float("inf"), float("nan")
+    for got, want in zip(ops.balance_loss(garbage, ids, mask=mask), ops.balance_loss(logits, ids, mask=mask)):
+        assert t.equal(got, want)
+    _, counts, _, rows = ops.balance_loss(logits, ids, mask=mask)
+    one = t.ones((), device="cuda")
+    assert t.equal(ops.balance_loss_backward(garbage, counts, rows, one, mask=mask), ops.balance_loss_backward(logits, counts, rows, one, mask=mask))
+    whole = t.full((tokens * 2, experts + 5), float("nan"), dtype=logits.dtype, device="cuda")
+    for view in (whole[::2, 1:experts + 1], whole[:tokens, 4:experts + 4], whole[tokens:, :experts]):
+        view.copy_(logits)
+        for got, want in zip(ops.balance_loss(view, ids, mask=mask), ops.balance_loss(logits, ids, mask=mask)):
+            assert t.equal(got, want)
+        assert t.equal(ops.balance_loss_backward(view, counts, rows, one, mask=mask), ops.balance_loss_backward(logits, counts, rows, one, mask=mask))
+
+
+def _balance_checked(ops, rng, logits, ids, mask, dtype):
+    t = _torch()
+    tokens, experts = logits.shape
     loss, counts, probs, rows = ops.balance_loss(logits, ids, mask=mask)
     m = None if mask is None else mask.cpu().numpy()
     wl, wc, wp, wr = O.balance(_np(logits), ids.cpu().numpy(), m)

@@ -64,16 +64,17 @@ assert attempt(W, M, M, M, M, 4, 2, 4, 4, M, M + 1, 0) == EI
 assert attempt(W, M, M, M, M, 1 << 23, 2, 4, 4, M, M, 0) == EU           # blocks
 assert attempt(W, None, None, None, None, 0, 2, 4, 4, M, M, 0) == 1      # no rows: zeros
 B = P.pccl_moe_balance
-space = P.pccl_moe_balance_workspace(h, 100, 8)
-ok = (M, 0, 100, 8, 8, M, 2, None, M, M, M, M)
-assert attempt(B, *ok, M, space) == 1 and attempt(B, M, 0, 1000, 8, 8, M, 2, None, M, M, M, M, M, 1 << 30) == 2
+space = P.pccl_moe_balance_workspace(h, 1000, 8)
+assert P.pccl_moe_balance_workspace(h, 100, 8) == 0 and attempt(B, M, 0, 100, 8, 8, M, 2, None, M, M, M, M) == 1   # one launch
+ok = (M, 0, 1000, 8, 8, M, 2, None, M, M, M, M)
+assert attempt(B, *ok, M, space) == 2
 assert attempt(B, *ok, M, space - 1) == EM and attempt(B, *ok) == EI and attempt(B, *ok, M + 4, space) == EI
 for i, bad, want in ((1, 9, EI), (3, 0, EI), (3, 1025, EU), (4, 7, EI), (5, None, EI), (6, 0, EI), (6, 9, EI), (8, None, EI), (9, None, EI), (10, None, EI), (11, M + 2, EI)):
     args = list(ok)
     args[i] = bad
     assert attempt(B, *args, M, space) == want, (i, bad)
 assert attempt(B, M, 0, 100, 1025, 1025, M, 2, None, M, M, M, M, M, 1 << 30) == EU
-assert attempt(B, None, 0, 0, 8, 8, None, 2, None, M, M, M, M, M, space) == 1   # no tokens: zeros
+assert attempt(B, None, 0, 0, 8, 8, None, 2, None, M, M, M, M) == 1   # no tokens: zeros
 K = P.pccl_moe_balance_backward
 assert attempt(K, M, 0, 4, 8, 8, None, M, M, M, None, M, 8) == 1 and attempt(K, M, 0, 4, 8, 8, None, M, M, None, None, M, 8) == 1
 assert attempt(K, M, 0, 4, 8, 8, None, None, M, M, None, M, 8) == EI and attempt(K, M, 0, 4, 8, 8, None, M, None, M, None, M, 8) == EI
