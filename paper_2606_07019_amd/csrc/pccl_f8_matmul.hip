@@ -168,7 +168,7 @@ __device__ inline void deal(uint32_t id, uint32_t mt, uint32_t nt, uint32_t &m, 
 // a whole stage's time.  In LDS chunk c (16 bytes) of row r stands at chunk c ^ (r
 // / 2 % 8) of the row, so the 16 lanes that read one chunk of 16 rows meet every
 // bank once.
-// 8192^3 takes 391 us, 2.8 PFLOP/s: the matrix units are busy 74 % of the cycles
+// 8192^3 takes 391 to 430 us by the clock of the run, 2.6 to 2.8 PFLOP/s: the matrix units are busy 74 % of the cycles
 // (the instruction alone reaches 4.0), the rest are meetings and 12 us a tile of
 // first copies and stores.  With results of 32 bits 770 us, 1.4 PFLOP/s, bound by
 // the matrix units' 16-bit rate.  EXPERTS: bound by reading the weights where an
