@@ -175,7 +175,7 @@ __device__ inline void deal(uint32_t id, uint32_t mt, uint32_t nt, uint32_t &m, 
 // expert has few rows (512 rows of 64 experts, 2048 x 2048, 41 us, 6.5 TB/s), by the
 // products where it has many (32,768 rows, 4096 x 2048, 359 us, 1.5 PFLOP/s: one
 // expert's last block is half empty).  GRADIENT: bound by storing (61 experts, 1000 x
-// 2040 of f32, from 12,297 rows, 146 us, 3.4 TB/s), each tile's few stages before it
+// 2040 of f32, from 12,297 rows, 144 us, 3.5 TB/s), each tile's few stages before it
 // (without the stores 105).
 // Tiles of 128 x 128 wait for their copies: 2048 x 4096 x 8192 takes 78 us, 68 without
 // the products, 52 without the copies; eight waves a tile change nothing.
@@ -366,20 +366,24 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy outlives the workgroup's LDS
     }
-    // The sums go through LDS, 32 rows of the wave's at a time, so that whole rows
-    // of them are stored, past the caches that the operands are read from (with
-    // ordinary stores 8192^3 takes 3 % longer, the gradient of 61 experts, 1000 x 2040 of
-    // f32, 46 %).  Few instructions a chunk, as a wave has a SIMD to itself (checks of
-    // every chunk's columns cost that gradient 5 %).  Rows of it that begin inside a
-    // line of 128 bytes cost 20 %; their first and last lines kept in the caches, more.
+    // The sums go through LDS, 32 rows of the waves beside each other at a time, so
+    // that a tile's whole rows are stored, past the caches that the operands are read
+    // from (with ordinary stores 8192^3 takes 3 % longer, the gradient of 61 experts,
+    // 1000 x 2040 of f32, 46 %).  Rows that begin inside a line of 128 bytes share
+    // their first and last with a neighbouring tile, which costs 8 % of that gradient
+    // (rows of single waves stored by themselves 15 %; those lines kept in the caches,
+    // more).  Few instructions a chunk, as a wave has a SIMD to itself (checks of every
+    // chunk's columns: 5 %).
     typedef u32x4 Chunk __attribute__((aligned(2)));   // at any address
     T *out = static_cast<T *>(a.out) + (KIND == EXPERTS ? 0u : (uint64_t)job.slice * a.m * a.ld);
-    constexpr uint32_t COLS = BN / WN, EACH = 16 / sizeof(T), CHUNKS_ROW = COLS / EACH, ROW = COLS * sizeof(T) + 16;
-    static_assert(WM * WN * 32 * ROW <= ALL, "within the stages' room");
+    constexpr uint32_t EACH = 16 / sizeof(T), CHUNKS_ROW = BN / EACH, ROW = BN * sizeof(T) + 16;
+    constexpr uint32_t EACH_PASS = 64 / CHUNKS_ROW, PASSES = 32 / WN / EACH_PASS;   // rows of a pass, passes
+    static_assert(2 * WM * 32 * ROW <= ALL, "within the stages' room");
+    const uint32_t row = wave % WN * (32 / WN) + lane / CHUNKS_ROW, n = lane % CHUNKS_ROW * EACH;
     __syncthreads();   // all have read the last stage
-    uint8_t *own = lds + wave * (32u * ROW);
 #pragma unroll
     for (int i = 0; i < TM; i++) {
+        uint8_t *rows = lds + (i % 2 * WM + wave / WN) * (32u * ROW);
 #pragma unroll
         for (int j = 0; j < TN; j++)
 #pragma unroll
@@ -387,13 +391,12 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
                 T t[4];
 #pragma unroll
                 for (int c = 0; c < 4; c++) t[c] = Elem<T>::put(acc[i][j][4 * q + c]);
-                __builtin_memcpy(__builtin_assume_aligned(own + r * ROW + (j * 32u + q * 8u + half * 4u) * sizeof(T), sizeof t), t, sizeof t);
+                __builtin_memcpy(__builtin_assume_aligned(rows + r * ROW + (wn + j * 32u + q * 8u + half * 4u) * sizeof(T), sizeof t), t, sizeof t);
             }
-        constexpr uint32_t PASSES = CHUNKS_ROW / 2, EACH_PASS = 64 / CHUNKS_ROW;   // rows of a pass
-        const uint32_t row = lane / CHUNKS_ROW, n = wn + lane % CHUNKS_ROW * EACH;
+        all_read();   // and what was written is there
         Chunk w[PASSES];
 #pragma unroll
-        for (uint32_t p = 0; p < PASSES; p++) w[p] = *reinterpret_cast<const u32x4 *>(own + (p * EACH_PASS + row) * ROW + lane % CHUNKS_ROW * 16u);
+        for (uint32_t p = 0; p < PASSES; p++) w[p] = *reinterpret_cast<const u32x4 *>(rows + (p * EACH_PASS + row) * ROW + lane % CHUNKS_ROW * 16u);
         const uint32_t m = wm + i * 32u + row, left = m < job.rows_a ? job.rows_a - m : 0u;
         T *to = out + (job.row + m) * a.ld + job.col + n;
         if (n + EACH <= job.rows_b) {
