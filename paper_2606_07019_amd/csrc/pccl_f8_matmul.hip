@@ -92,16 +92,16 @@ __device__ inline void mixed()
     }
 }
 
-// Four neighbouring sums of row `row`, from column `col` on.
+// Four neighbouring sums of row `row`, from column `col` on, to any address.
 template <class T>
-__device__ inline void store4(T *out, uint64_t ld, uint64_t row, uint64_t col, uint64_t n, f32x4 v, bool vec)
+__device__ inline void store4(T *out, uint64_t ld, uint64_t row, uint64_t col, uint64_t n, f32x4 v)
 {
     T t[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) t[i] = Elem<T>::put(v[i]);
     T *p = out + row * ld + col;
-    if (vec && col + 4 <= n) {
-        __builtin_memcpy(__builtin_assume_aligned(p, sizeof t), t, sizeof t);
+    if (col + 4 <= n) {
+        __builtin_memcpy(p, t, sizeof t);
         return;
     }
 #pragma unroll
@@ -438,11 +438,11 @@ __device__ inline f32x4 product16(const Piece &y, uint32_t ys, const Piece &x, u
 }
 
 // Four neighbouring sums of row `row`, in the output's type.
-__device__ inline void store4_as(void *out, uint32_t dtype, uint64_t ld, uint64_t row, uint64_t col, uint64_t n, f32x4 v, bool vec)
+__device__ inline void store4_as(void *out, uint32_t dtype, uint64_t ld, uint64_t row, uint64_t col, uint64_t n, f32x4 v)
 {
-    if (dtype == DT_F32) store4(static_cast<float *>(out), ld, row, col, n, v, vec);
-    else if (dtype == DT_BF16) store4(static_cast<__bf16 *>(out), ld, row, col, n, v, vec);
-    else store4(static_cast<_Float16 *>(out), ld, row, col, n, v, vec);
+    if (dtype == DT_F32) store4(static_cast<float *>(out), ld, row, col, n, v);
+    else if (dtype == DT_BF16) store4(static_cast<__bf16 *>(out), ld, row, col, n, v);
+    else store4(static_cast<_Float16 *>(out), ld, row, col, n, v);
 }
 
 constexpr uint32_t SLOT = 2048 + 256;   // a step of 16 rows, and the words of their scales
@@ -459,7 +459,7 @@ constexpr uint32_t few_lds() { return WAVES * D * SLOT + 2 * WAVES * MT * 1024; 
 // that as many copies are under way.  48 x 16384 x 5120 takes 22.5 us from memory, 3.7
 // TB/s (the tiles' form 26.6), 16.9 from the device's cache; 1 x 4096 x 4096 6.3 (14.3).
 template <bool EXACT, int MT, int S, int WAVES, int D>
-__global__ __launch_bounds__(64 * WAVES) void k_f8_few(F8MatmulArgs a, uint32_t dtype, bool vec, uint32_t tiles)
+__global__ __launch_bounds__(64 * WAVES) void k_f8_few(F8MatmulArgs a, uint32_t dtype, uint32_t tiles)
 {
     extern __shared__ __align__(16) uint8_t lds[];
     const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -567,7 +567,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_f8_few(F8MatmulArgs a, uint32_t 
 #pragma unroll
             for (uint32_t q = 1; q < WAVES; q++) v += part[(q * MT + wave) * 64u + lane];
             const uint32_t m = wave * 16u + r;
-            if (m < rows) store4_as(out, dtype, a.ld, m, ((uint64_t)blockIdx.x + (uint64_t)i * gridDim.x) * 16u + g * 4u, a.n, v, vec);
+            if (m < rows) store4_as(out, dtype, a.ld, m, ((uint64_t)blockIdx.x + (uint64_t)i * gridDim.x) * 16u + g * 4u, a.n, v);
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy outlives the workgroup's LDS
@@ -576,14 +576,14 @@ __global__ __launch_bounds__(64 * WAVES) void k_f8_few(F8MatmulArgs a, uint32_t 
 // The sums of a shared-out k, joined in the order of its parts: a thread takes
 // four columns of a row.  Rows of the parts are padded to `ld`, whole fours.
 template <class T>
-__global__ __launch_bounds__(256) void k_f8_join(F8MatmulArgs a, uint32_t splits, uint64_t ld, bool vec)
+__global__ __launch_bounds__(256) void k_f8_join(F8MatmulArgs a, uint32_t splits, uint64_t ld)
 {
     const uint64_t i = (uint64_t)blockIdx.x * 256u + threadIdx.x, row = i / (ld / 4), col = i % (ld / 4) * 4u;
     if (row >= a.m) return;
     const float *p = a.part + row * ld + col;
     f32x4 v = *reinterpret_cast<const f32x4 *>(p);
     for (uint32_t j = 1; j < splits; j++) v += *reinterpret_cast<const f32x4 *>(p + (uint64_t)j * a.m * ld);
-    store4(static_cast<T *>(a.out), a.ld, row, col, a.n, v, vec);
+    store4(static_cast<T *>(a.out), a.ld, row, col, a.n, v);
 }
 
 template <class T, bool EXACT, Kind KIND, int BM, int BN, int WM, int WN, int BUFFERS>
@@ -672,10 +672,8 @@ hipError_t few_as(const F8MatmulArgs &a, uint32_t dtype, uint32_t slices, uint32
     static_assert(bytes <= 160u << 10 && MT * S <= 16, "one workgroup's LDS, and registers");
     const hipError_t e = allow_lds<&k_f8_few<EXACT, MT, S, WAVES, D>>(bytes);
     if (e != hipSuccess) return e;
-    const size_t elem = dtype == DT_F32 ? 4 : 2;
-    const bool vec = (reinterpret_cast<uintptr_t>(a.out) | (a.ld * elem)) % (4 * elem) == 0;
     const uint32_t tiles = (uint32_t)((a.n + 15) / 16);
-    k_f8_few<EXACT, MT, S, WAVES, D><<<dim3(tiles < workers ? tiles : workers, slices), 64 * WAVES, bytes, s>>>(a, dtype, vec, tiles);
+    k_f8_few<EXACT, MT, S, WAVES, D><<<dim3(tiles < workers ? tiles : workers, slices), 64 * WAVES, bytes, s>>>(a, dtype, tiles);
     return hipGetLastError();
 }
 
@@ -695,8 +693,7 @@ template <class T>
 hipError_t join(const F8MatmulArgs &a, uint32_t parts, hipStream_t s)
 {
     const uint64_t ld = padded(a.n), threads = a.m * (ld / 4);
-    const bool vec = (reinterpret_cast<uintptr_t>(a.out) | (a.ld * sizeof(T))) % (4 * sizeof(T)) == 0;
-    k_f8_join<T><<<dim3((uint32_t)((threads + 255) / 256)), 256, 0, s>>>(a, parts, ld, vec);
+    k_f8_join<T><<<dim3((uint32_t)((threads + 255) / 256)), 256, 0, s>>>(a, parts, ld);
     return hipGetLastError();
 }
 
