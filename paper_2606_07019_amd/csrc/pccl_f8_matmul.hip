@@ -10,7 +10,8 @@
 // values the results' error is 1.4e-5 of their norm, 4.4e-5 with a value twenty
 // times the others in every row: a hundredth of what rounding to bf16 costs, a
 // tenth of f16.  Results of 32 bits are summed in 32 bits: codes become bf16,
-// scaled, which is exact, for the 16-bit form (32 rows over 16 values of k).
+// scaled, which is exact between 2^-126 and 2^128, for the 16-bit form (32 rows
+// over 16 values of k); blocks beyond 2^128 are summed unscaled.
 //
 // Either form has lane l of a wave give row l % 32 of an operand, and sixteen
 // sums, four neighbours in rows 8 q + 4 (l / 32) of the first operand, row l %
@@ -37,6 +38,35 @@ __device__ inline bf16x8 wide(uint32_t w0, uint32_t w1, float scale)
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true);
     const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true);
     return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+
+// The lowest scale byte with which a block's largest codes pass bf16's numbers: 256 * 2^120 does.
+// A wave that meets one makes its sums anew (the check for it: 8192^3 835 us with it,
+// 831 without, 64 x 4096 x 4096 11.6 and 11.5).
+constexpr uint32_t BEYOND = 247;
+
+// A sum of products of codes with both scales; ldexp takes them to where the sum lies, whatever each of them is.
+__device__ inline float with_scales(float sum, uint32_t xs, uint32_t ys)
+{
+    return xs == 255u || ys == 255u ? __uint_as_float(0x7FC00000u) : ldexpf(sum, (int)(xs + ys) - 254);
+}
+
+// c += y x over a block of 128 values, its scales applied to its sum, as blocks
+// beyond what bf16 holds need it.  Lane l has 64 codes of row l % 32 of either.
+__device__ inline void add_unscaled(f32x16 &c, const uint8_t *x, uint32_t xs, const uint8_t *y, uint32_t ys)
+{
+    f32x16 sum = {};
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        const u32x4 v = reinterpret_cast<const u32x4 *>(y)[q], w = reinterpret_cast<const u32x4 *>(x)[q];
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide(v.x, v.y, 1.f), wide(w.x, w.y, 1.f), sum, 0, 0, 0);
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide(v.z, v.w, 1.f), wide(w.z, w.w, 1.f), sum, 0, 0, 0);
+    }
+#pragma unroll
+    for (int q = 0; q < 16; q++) {
+        const int row = q / 4 * 8 + q % 4;   // of y: 4 more in the upper half of the lanes
+        c[q] += with_scales(sum[q], xs, (uint32_t)__shfl((int)ys, row + (int)(threadIdx.x & 32u) / 8));
+    }
 }
 
 // c[i][j] += y[j] x[i] over 64 values of k, for products FROM up to TO in the
@@ -324,6 +354,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
     auto held_back = []() { asm volatile("" ::: "memory"); };
     constexpr int N = TM * TN, READS = 2 * (TM + TN), PART = EXACT ? N / 4 : N * 3 / 8, CUT = EXACT ? COPIES / 2 : COPIES * 3 / 4;   // products of a step, its reads; what the second part takes
     f32x16 acc[TM][TN] = {};
+    uint32_t top = 0;   // EXACT: the largest scale byte
     if (stages) {
         copy_scales(job.first / 4u);
         copy_scales(job.first / 4u + 1u);
@@ -339,6 +370,12 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
         for (uint32_t s = 0; s < stages; s++) {
             held_back();
             const Scales now = bytes_of(words, s);
+            if constexpr (EXACT) {
+#pragma unroll
+                for (int i = 0; i < TM; i++) top = max(top, now.x[i] & 0xFFu);
+#pragma unroll
+                for (int j = 0; j < TN; j++) top = max(top, now.y[j] & 0xFFu);
+            }
 #pragma unroll
             for (int q = 0; q < TM + TN; q++) read(held[1], s, 1, q);
             products<EXACT, 0, N - PART>(acc, held[0].x, now.x, held[0].y, now.y);
@@ -366,6 +403,19 @@ __global__ __launch_bounds__(64 * WM * WN) void k_f8_product(F8MatmulArgs a, uin
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy outlives the workgroup's LDS
     }
+    if constexpr (EXACT)
+        if (__any(top >= BEYOND)) {   // the wave's sums again, from memory
+#pragma unroll
+            for (int i = 0; i < TM; i++)
+#pragma unroll
+                for (int j = 0; j < TN; j++) {
+                    const uint32_t mx = wm + i * 32u + r, my = wn + j * 32u + r, rx = mx < lm ? mx : lm, ry = my < ln ? my : ln;
+                    f32x16 sum = {};
+                    for (uint32_t k = job.first; k < job.first + stages; k++)
+                        add_unscaled(sum, job.a + (rx * cb + k * 128u + half * 64u), job.as[rx * sb + k], job.b + (ry * cb + k * 128u + half * 64u), job.bs[ry * sb + k]);
+                    acc[i][j] = sum;
+                }
+        }
     // The sums go through LDS, 32 rows of the waves beside each other at a time, so
     // that a tile's whole rows are stored, past the caches that the operands are read
     // from (with ordinary stores 8192^3 takes 3 % longer, the gradient of 61 experts,
@@ -435,6 +485,20 @@ __device__ inline f32x4 product16(const Piece &y, uint32_t ys, const Piece &x, u
         auto whole = [](const Piece &p) { return i32x8{(int)p.lo.x, (int)p.lo.y, (int)p.lo.z, (int)p.lo.w, (int)p.hi.x, (int)p.hi.y, (int)p.hi.z, (int)p.hi.w}; };
         return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(y), whole(x), c, 0, 0, 0, (int)ys, 0, (int)xs);
     }
+}
+
+// c += y x over a block, its scales applied to its sum: for blocks beyond what bf16 holds.
+__device__ inline void add_unscaled16(f32x4 &c, const uint8_t *x, uint32_t xs, const uint8_t *y, uint32_t ys)
+{
+    f32x4 sum = {};
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const u32x4 v = reinterpret_cast<const u32x4 *>(y)[q], w = reinterpret_cast<const u32x4 *>(x)[q];
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide(v.x, v.y, 1.f), wide(w.x, w.y, 1.f), sum, 0, 0, 0);
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide(v.z, v.w, 1.f), wide(w.z, w.w, 1.f), sum, 0, 0, 0);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; q++) c[q] += with_scales(sum[q], xs, (uint32_t)__shfl((int)ys, (int)(threadIdx.x & 48u) / 4 + q));
 }
 
 // Four neighbouring sums of row `row`, in the output's type.
@@ -535,6 +599,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_f8_few(F8MatmulArgs a, uint32_t 
             else issue_b((uint32_t)(t + (j + D) / S - MT), (j + D) % S, slot);
             next();
         });
+    uint32_t top = 0;   // EXACT: the largest scale byte of A
+    if constexpr (EXACT) {
+#pragma unroll
+        for (uint32_t j = 0; j < S; j++)
+#pragma unroll
+            for (int t = 0; t < MT; t++) top = j < mine ? max(top, xs[t][j]) : top;
+    }
     for (uint32_t i = 0; i < mine_tiles; i++) {
         f32x4 acc[MT] = {};
         uint32_t ys[S];
@@ -556,6 +627,21 @@ __global__ __launch_bounds__(64 * WAVES) void k_f8_few(F8MatmulArgs a, uint32_t 
                     }
             }
         });
+        if constexpr (EXACT) {
+            uint32_t most = top;
+#pragma unroll
+            for (uint32_t j = 0; j < S; j++) most = j < mine ? max(most, ys[j]) : most;
+            if (__any(most >= BEYOND)) {   // the wave's sums again, from memory
+                const uint64_t n = ((uint64_t)blockIdx.x + (uint64_t)i * gridDim.x) * 16u + r, ry = n < a.n ? n : a.n - 1;
+#pragma unroll
+                for (int t = 0; t < MT; t++) {
+                    const uint64_t m = t * 16u + r, rx = m < rows ? m : rows - 1u;
+                    acc[t] = f32x4{};
+                    for (uint32_t k = s0; k < s0 + mine; k++)
+                        add_unscaled16(acc[t], a.a + (rx * cb + k * 128u + g * 32u), a.as[rx * sb + k], a.b + (ry * cb + k * 128u + g * 32u), a.bs[ry * sb + k]);
+                }
+            }
+        }
         f32x4 *part = sums + (i % 2u) * (WAVES * MT * 64u);
 #pragma unroll
         for (int t = 0; t < MT; t++) part[(wave * MT + t) * 64u + lane] = acc[t];
