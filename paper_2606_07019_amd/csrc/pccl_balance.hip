@@ -366,7 +366,7 @@ __global__ __launch_bounds__(BACK_THREADS) void k_balance_backward(BalanceBackwa
     typedef Share<T, LANES, V> Mine;
     int32_t c[V];
     float g[V];
-    uint32_t picks = 0;
+    uint32_t low = 0, high = 0;   // of the picks: ranks' counts together may pass 32 bits
 #pragma unroll
     for (int i = 0; i < V; i += Mine::PIECE) {
         const uint32_t e = Mine::expert(sub, i);
@@ -382,8 +382,12 @@ __global__ __launch_bounds__(BACK_THREADS) void k_balance_backward(BalanceBackwa
         }
     }
 #pragma unroll
-    for (int i = 0; i < V; i++) picks += (uint32_t)c[i];
-    picks = reduce<LANES>(picks, [](uint32_t a, uint32_t b) { return a + b; });
+    for (int i = 0; i < V; i++) {
+        low += (uint32_t)c[i] & 0xFFFFu;
+        high += (uint32_t)c[i] >> 16;
+    }
+    auto add = [](uint32_t a, uint32_t b) { return a + b; };
+    const uint64_t picks = ((uint64_t)reduce<LANES>(high, add) << 16) + reduce<LANES>(low, add);
     const float each = rows ? 1.f / (float)rows : 0.f;
     const float unit = picks ? dloss * ((float)a.experts / (float)picks) : 0.f;
 #pragma unroll

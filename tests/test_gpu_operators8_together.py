@@ -149,3 +149,34 @@ def test_products_bump_the_version_of_what_they_write(ops):   # noqa: F811
     with t.inference_mode():
         ops.matmul8(q, q, t.float32, out=t.zeros(70, 70, device="cuda"))
     assert not ops.quantize8(x.float().requires_grad_()).codes.requires_grad
+
+
+@pytest.mark.parametrize("experts", [8, 200, 600])
+def test_gradient_of_a_joint_batch(ops, experts):   # noqa: F811
+    """Counts and rows summed over ranks: more picks in all than 32 bits hold."""
+    print(f"[operators8] joint batch, {experts} experts", flush=True)
+    t = _torch()
+    rng = np.random.default_rng(experts)
+    logits = _to(rng.normal(size=(70, experts)) * 2, "f32")
+    counts = rng.integers(0, 2 ** 31, size=experts).astype(np.int32)
+    counts[:3] = 2 ** 31 - 1
+    rows, dloss = 2 ** 30 + 7, 2.0 ** 30
+    got = _np(ops.balance_loss_backward(logits, t.from_numpy(counts).cuda(), t.tensor(rows, dtype=t.int32, device="cuda"),
+                                        t.full((), dloss, device="cuda")))
+    assert counts.astype(np.int64).sum() > 2 ** 32
+    want = O.balance_backward(_np(logits), counts, rows, dloss)
+    p = np.exp(_np(logits))
+    p /= p.sum(axis=1, keepdims=True)
+    size = dloss * experts * counts / counts.astype(np.float64).sum()
+    # as in tests/test_gpu_operators8.py: a probability's error, and the difference's, as large as its parts
+    bound = p * (size + (p * size).sum(axis=1, keepdims=True)) / rows * (2.0 ** 5 + 2 * experts + 16) * 2.0 ** -24
+    assert (np.abs(got - want) <= bound + 2.0 ** -24 * np.abs(want)).all()
+    # and the halves of a batch, each with the counts and rows of both, have the gradient of the whole
+    ids = t.from_numpy(rng.integers(0, experts, (70, 2)).astype(np.int32)).cuda()
+    _, whole, _, n = ops.balance_loss(logits, ids)
+    one = t.ones((), device="cuda")
+    parts = [ops.balance_loss(logits[i:i + 35], ids[i:i + 35].contiguous()) for i in (0, 35)]
+    joint, both = parts[0][1] + parts[1][1], parts[0][3] + parts[1][3]
+    assert t.equal(joint, whole) and t.equal(both, n)
+    halves = [ops.balance_loss_backward(logits[i:i + 35], joint, both, one) for i in (0, 35)]
+    assert t.equal(t.cat(halves), ops.balance_loss_backward(logits, whole, n, one))
