@@ -11,7 +11,7 @@ Of torch's automatic differentiation, route()'s weights carry the router's
 gradient, and balance_loss()'s loss and probabilities theirs.  Packed values are
 whole numbers and have none: a training step makes its three products itself, of
 operands packed along the axis that each sums over.  moe_layer() is for serving;
-asked for a gradient, its result raises.
+asked for a gradient, its result raises, as that of balance_loss_backward() does.
 
     ops = Operators()
     q = ops.quantize(x)                          # rows in 4.25 bits a value
@@ -138,11 +138,11 @@ class _Balance(torch.autograd.Function):
             return None, None, None, None
         if dprobs is not None:
             dprobs = dprobs.contiguous()
-        return ctx.ops.balance_loss_backward(logits, counts, rows, dloss, dprobs, mask), None, None, None
+        return ctx.ops._balance_backward(logits, dloss, dprobs, counts, rows, mask), None, None, None
 
 
 class _Served(torch.autograd.Function):
-    """A result without a gradient, for inputs that a gradient is asked of."""
+    """A result without a gradient, for inputs that one is recorded for: silence would end their graph."""
 
     @staticmethod
     def forward(ctx, name, call, *inputs):
@@ -378,6 +378,11 @@ class Operators:
         """The gradient of balance_loss()'s loss and probs with respect to its
         logits, in their type.  With counts and rows summed over ranks it is this
         rank's part of the gradient of the loss of their joint batch."""
+        if _learns(*(t for t in (logits, dloss, dprobs) if t is not None)):
+            return _Served.apply("balance_loss_backward", lambda *given: self._balance_backward(*given, counts, rows, mask), logits, dloss, dprobs)
+        return self._balance_backward(logits, dloss, dprobs, counts, rows, mask)
+
+    def _balance_backward(self, logits, dloss, dprobs, counts, rows, mask):
         tokens, experts, ld = self._matrix("logits", logits)
         out = self._empty(logits.dtype, tokens, experts)
         self._call(
