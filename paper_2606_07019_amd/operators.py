@@ -11,7 +11,8 @@ Of torch's automatic differentiation, route()'s weights carry the router's
 gradient, and balance_loss()'s loss and probabilities theirs.  Packed values are
 whole numbers and have none: a training step makes its three products itself, of
 operands packed along the axis that each sums over.  moe_layer() is for serving;
-asked for a gradient, its result raises, as that of balance_loss_backward() does.
+asked for a gradient, its result raises, as those of route_backward() and
+balance_loss_backward() do.
 
     ops = Operators()
     q = ops.quantize(x)                          # rows in 4.25 bits a value
@@ -89,11 +90,11 @@ def _group_words(experts, rows):
 
 
 def _learns(*tensors):
-    """Whether a derivative is recorded for one of the tensors; RuntimeError for a forward-mode one, which none has here."""
-    if forward_ad._current_level >= 0 and any(forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+    """Whether a derivative is recorded for one of the tensors (or None); RuntimeError for a forward-mode one, which none has here."""
+    if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
         raise RuntimeError("the operators have no forward-mode derivatives")
     for t in tensors:
-        if t.requires_grad:
+        if t is not None and t.requires_grad:
             return torch.is_grad_enabled()
     return False
 
@@ -335,6 +336,9 @@ class Operators:
     def route_backward(self, logits, weights, ids, dweights, normalize: bool = True,
                        mask: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The gradient of route()'s weights with respect to its logits, in their type."""
+        if _learns(logits, weights, dweights):
+            return _Served.apply("route_backward", lambda l, w, d: self._route_backward(l, l.shape, l.dtype, w, ids, d, normalize, mask),
+                                 logits, weights, dweights)
         return self._route_backward(logits, logits.shape, logits.dtype, weights, ids, dweights, normalize, mask)
 
     def _route_backward(self, logits, shape, dtype, weights, ids, dweights, normalize, mask):
@@ -378,7 +382,7 @@ class Operators:
         """The gradient of balance_loss()'s loss and probs with respect to its
         logits, in their type.  With counts and rows summed over ranks it is this
         rank's part of the gradient of the loss of their joint batch."""
-        if _learns(*(t for t in (logits, dloss, dprobs) if t is not None)):
+        if _learns(logits, dloss, dprobs):
             return _Served.apply("balance_loss_backward", lambda *given: self._balance_backward(*given, counts, rows, mask), logits, dloss, dprobs)
         return self._balance_backward(logits, dloss, dprobs, counts, rows, mask)
 

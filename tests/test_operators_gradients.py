@@ -27,7 +27,13 @@ def _balance(ops, learned):
     return lambda: ops.balance_loss_backward(given["logits"], torch.ones(8, dtype=i32), torch.ones((), dtype=i32), given["dloss"], given["dprobs"])
 
 
-CALLS = [(_balance, n) for n in ("logits", "dloss", "dprobs")]
+def _route(ops, learned):
+    given = {"logits": torch.zeros(6, 8), "weights": torch.zeros(6, 2), "dweights": torch.ones(6, 2)}
+    given = {k: v.requires_grad_() if k == learned else v for k, v in given.items()}
+    return lambda: ops.route_backward(given["logits"], given["weights"], torch.zeros(6, 2, dtype=torch.int32), given["dweights"], normalize=False)
+
+
+CALLS = [(_balance, n) for n in ("logits", "dloss", "dprobs")] + [(_route, n) for n in ("logits", "weights", "dweights")]
 
 
 @pytest.mark.parametrize("make,learned", CALLS, ids=[f"{f.__name__[1:]}-{n}" for f, n in CALLS])
@@ -63,5 +69,11 @@ def test_recorded_gradients_are_as_they_were(ops):
 def test_forward_mode_is_refused(ops):
     from torch.autograd import forward_ad
     x = torch.zeros(6, 8)
-    with forward_ad.dual_level(), pytest.raises(RuntimeError, match="forward-mode"):
-        ops.balance_loss_backward(forward_ad.make_dual(x, x), torch.ones(8, dtype=torch.int32), torch.ones((), dtype=torch.int32), torch.ones(()))
+    i32 = torch.int32
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, x)
+        with pytest.raises(RuntimeError, match="forward-mode"):
+            ops.balance_loss_backward(dual, torch.ones(8, dtype=i32), torch.ones((), dtype=i32), torch.ones(()))
+        with pytest.raises(RuntimeError, match="forward-mode"):
+            ops.route_backward(dual, x[:, :2].contiguous(), torch.zeros(6, 2, dtype=i32), x[:, :2].contiguous())
+        assert not ops.balance_loss_backward(x, torch.ones(8, dtype=i32), torch.ones((), dtype=i32), None, torch.ones(8)).requires_grad
