@@ -41,8 +41,10 @@ __device__ inline bf16x8 wide(uint32_t w0, uint32_t w1, float scale)
 }
 
 // The lowest scale byte with which a block's largest codes pass bf16's numbers: 256 * 2^120 does.
-// A wave that meets one makes its sums anew (the check for it: 8192^3 835 us with it,
-// 831 without, 64 x 4096 x 4096 11.6 and 11.5).
+// A wave that meets one makes its sums anew (with that and without, in us, where none
+// does: 8192^3 783 and 784, 2040 x 2080 x 1500 22.0 and 21.7, 64 x 4096 x 4096 11.6 and
+// 11.5; made anew behind the stores, so that the loop's registers stay as they were:
+// 788, 22.1 and 11.6).
 constexpr uint32_t BEYOND = 247;
 
 // A sum of products of codes with both scales; ldexp takes them to where the sum lies, whatever each of them is.
@@ -837,10 +839,12 @@ hipError_t launch_f8_expert_matmul(const F8MatmulArgs &a, uint32_t dtype, hipStr
         typedef decltype(t) T;
         constexpr bool EXACT = sizeof(T) == 4;
         // an expert's last block is half full, as far as one can know here (large and
-        // small: 32,768 rows of 64 experts, 4096 x 2048, 359 and 394 us; 512 rows, 2048 x
-        // 2048, 55 and 42)
-        const uint64_t half = a.experts / 2, small = (a.rows / 128 + half) * ((a.n + 127) / 128), large = (a.rows / 256 + half) * ((a.n + 255) / 256);
-        if (large_tiles(small, large, EXACT))
+        // small: 32,768 rows of 64 experts, 4096 x 2048, 359 and 394 us); with up to one small
+        // block an expert most of a large one is empty (128 rows of 64 experts, 2048 x 2048,
+        // 52 and 34; 4096 rows 90 and 63, 8192 rows 93 and 85; 192 rows of one, 4096 x 2048,
+        // 25 and 13)
+        const uint64_t half = a.experts / 2, small = ((a.rows + 127) / 128 + half) * ((a.n + 127) / 128), large = ((a.rows + 255) / 256 + half) * ((a.n + 255) / 256);
+        if (a.rows > 128ull * a.experts && large_tiles(small, large, EXACT))
             return product<T, EXACT, EXPERTS, 256, 256, 2, 2, 2>(a, (uint32_t)groups_blocks(a.experts, a.rows, 256), 1, 0, s);
         return product<T, EXACT, EXPERTS, 128, 128, 2, 2, 2>(a, (uint32_t)groups_blocks(a.experts, a.rows, 128), 1, 0, s);
     });
