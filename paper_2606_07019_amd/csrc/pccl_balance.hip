@@ -84,19 +84,19 @@ __device__ inline bool softmax(const T (&t)[V], bool there, float (&v)[V])
     return any;
 }
 
-// What the workgroups leave for the joining one: sums of probabilities
-// [groups][experts], counts [groups][experts], rows [groups]; a joining
-// workgroup's sum of counts and part of the loss; how many of them are done.
+// What the workgroups leave for the joining ones: sums of probabilities
+// [groups][experts], counts [groups][experts], rows [groups]; and how many of the
+// joining ones are done.
 struct Space {
-    float *probs, *loss;
+    float *probs;
     uint32_t *counts, *rows, *done;
 };
+constexpr uint32_t DONE_BYTES = 256;
 inline __host__ __device__ Space space_of(char *ws, uint32_t groups, uint32_t experts)
 {
     Space s;
     s.done = reinterpret_cast<uint32_t *>(ws);
-    s.loss = reinterpret_cast<float *>(ws) + 64;
-    s.rows = reinterpret_cast<uint32_t *>(ws) + 128;
+    s.rows = reinterpret_cast<uint32_t *>(ws + DONE_BYTES);
     s.probs = reinterpret_cast<float *>(s.rows + groups);
     s.counts = reinterpret_cast<uint32_t *>(s.probs) + (uint64_t)groups * experts;
     return s;
@@ -467,7 +467,7 @@ size_t balance_workspace(uint64_t tokens, uint32_t experts)
 {
     const uint64_t groups = workgroups(tokens, experts);
     if (groups == 1) return 0;
-    return (size_t)((512 + 4 * groups * (1 + 2 * (uint64_t)experts) + 255) & ~255ull);
+    return (size_t)((DONE_BYTES + 4 * groups * (1 + 2 * (uint64_t)experts) + 255) & ~255ull);
 }
 
 hipError_t launch_balance(const BalanceArgs &a, uint32_t dtype, hipStream_t s) { return by_type<Forward>(a, dtype, s); }

@@ -27,7 +27,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef const __attribute__((address_space(1))) void *gptr;
 typedef __attribute__((address_space(3))) void *lptr;
 
-// 32 bytes of a row, and the byte of its scale.
+// 32 codes of a row.
 struct Piece {
     u32x4 lo, hi;
 };
@@ -532,7 +532,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_f8_few(F8MatmulArgs a, uint32_t 
     const uint32_t r = lane & 15u, g = lane >> 4;
     const uint32_t cb = (uint32_t)f8_code_bytes(a.k), sb = (uint32_t)f8_scale_bytes(a.k), steps = (uint32_t)f8_blocks(a.k);
     const uint32_t s0 = (blockIdx.y * WAVES + wave) * S, mine = s0 < steps ? (steps - s0 < S ? steps - s0 : S) : 0u;
-    const uint32_t rows = (uint32_t)a.m, mts = (rows + 15u) / 16u;
+    const uint32_t rows = (uint32_t)a.m;   // more than 16 (MT - 1)
     char *out = static_cast<char *>(a.out) + (uint64_t)blockIdx.y * a.m * a.ld * sizeof(float);   // of the partial sums
     uint8_t *ring = lds + wave * (D * SLOT);
     f32x4 *sums = reinterpret_cast<f32x4 *>(lds + WAVES * D * SLOT);   // [2][WAVES][MT][64]
@@ -621,12 +621,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_f8_few(F8MatmulArgs a, uint32_t 
             next();
             if ((uint32_t)j < mine) {
 #pragma unroll
-                for (int t = 0; t < MT; t++)
-                    if ((uint32_t)t < mts) {
-                        // as codes, not as the twice as many registers of bf16 that they become anew for every tile
-                        if constexpr (EXACT) asm volatile("" : "+v"(x[t][j].lo), "+v"(x[t][j].hi));
-                        acc[t] = product16<EXACT>(y, ys[j], x[t][j], xs[t][j], acc[t]);
-                    }
+                for (int t = 0; t < MT; t++) {
+                    // as codes, not as the twice as many registers of bf16 that they become anew for every tile
+                    if constexpr (EXACT) asm volatile("" : "+v"(x[t][j].lo), "+v"(x[t][j].hi));
+                    acc[t] = product16<EXACT>(y, ys[j], x[t][j], xs[t][j], acc[t]);
+                }
             }
         });
         if constexpr (EXACT) {
