@@ -180,3 +180,37 @@ def test_gradient_of_a_joint_batch(ops, experts):   # noqa: F811
     assert t.equal(joint, whole) and t.equal(both, n)
     halves = [ops.balance_loss_backward(logits[i:i + 35], joint, both, one) for i in (0, 35)]
     assert t.equal(t.cat(halves), ops.balance_loss_backward(logits, whole, n, one))
+
+
+def test_two_streams_and_two_contexts_at_once(ops):   # noqa: F811
+    """Calls with workspaces in flight together, with nothing waited for in between."""
+    print("[operators8] two streams, two contexts", flush=True)
+    from paper_2606_07019_amd.operators import Operators
+    from test_gpu_operators8 import _packed
+    t = _torch()
+    rng = np.random.default_rng(10)
+    many = [_packed(rng, rows, 9000, 116, 122)[0] for rows in (129, 257)]   # shared out over k
+    few = [_packed(rng, rows, 20000, 116, 122)[0] for rows in (7, 3000)]
+    l = _to(rng.normal(size=(5000, 300)), "f32")                 # many workgroups, joined
+    ids = t.from_numpy(rng.integers(0, 300, (5000, 4)).astype(np.int32)).cuda()
+    inputs = _inputs(11)
+
+    def calls(o):
+        return [o.matmul8(*many, t.float32), o.matmul8(*few, t.bfloat16), *o.balance_loss(l, ids), o.matmul8(*few, t.float32),
+                o.matmul8(*many, t.bfloat16), *_step(o, *inputs)]
+
+    want = [a.clone() for a in calls(ops)]
+    other = Operators(0)
+    for contexts in ((ops, ops), (ops, other), (other, other)):
+        sides = [t.cuda.Stream() for _ in range(2)]
+        got = []
+        for side in sides:
+            side.wait_stream(t.cuda.current_stream())
+        for _ in range(4):
+            for side, o in zip(sides, contexts):
+                with t.cuda.stream(side):
+                    got.append(calls(o))
+        t.cuda.synchronize()
+        for results in got:
+            assert all(t.equal(a, b) for a, b in zip(results, want))
+    other.close()

@@ -27,3 +27,10 @@ print("as measured")
 
 def test_experts_of_few_rows_take_small_tiles(tmp_path):
     assert "as measured" in run_with_recorder(tmp_path, EXPERTS)
+
+
+def test_every_kernel_of_few_rows_is_run():
+    from test_gpu_operators8_steps import MADE, MOST, SHAPES, kernel
+    reached = {kernel(m, 128 * blocks) for m in (1, 20, 40, 60) for blocks in range(1, 4097)}
+    assert {kernel(m, k) for m, _, k in SHAPES} == reached
+    assert reached == {(rows, s) for rows, most in MOST.items() for s in MADE if s <= most}
