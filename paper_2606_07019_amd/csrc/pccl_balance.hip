@@ -60,8 +60,8 @@ struct Share {
 // (otherwise zeros).  Minus infinity is no expert; a NaN among the logits is lost
 // in the largest but not in the sum, and makes the row's NaN, as plus infinity does.
 // The instruction for 2^x as it is, without the library's steps for results below
-// 2^-126, which are zero here beside a largest of 1 (32,768 x 256 of bf16, both ways,
-// 26.5 us and 30.4 with expf).
+// 2^-126, which are zero here beside a largest of 1 (32,768 x 256 of bf16, forward pass
+// 14.6 us and 16.5 with expf, backward 11.5 and 13.6, each in a graph of its own).
 template <class T, int LANES, int V>
 __device__ inline bool softmax(const T (&t)[V], bool there, float (&v)[V])
 {
@@ -128,8 +128,10 @@ __device__ inline void over_all(uint32_t &u, float &f, uint32_t *us, float *fs)
 
 // LANES lanes a row, WAVES * 64 / LANES rows at a time; the next ones are read
 // while these are summed up.  One workgroup by itself makes the outputs, several
-// leave their sums to the joining kernels.  Bound by reading the logits and by the
-// exponentials: 32,768 x 256 of bf16 10.5 us (17 MB from the device's cache).
+// leave their sums to the joining kernels.  32,768 x 256 of bf16 9.2 to 10.8 us (17 MB
+// from the device's cache): of a compute unit's busy cycles vector instructions take
+// 57 %, the exponentials among them 11 %; waves wait 63 % of their time, for rows and
+// at the meetings of the end.
 template <class T, int LANES, int V>
 __global__ __launch_bounds__(THREADS) void k_balance(BalanceArgs a)
 {
@@ -336,8 +338,9 @@ __global__ __launch_bounds__(THREADS) void k_balance_join_many(BalanceArgs a, ui
 }
 
 // The softmax again, from the logits: reading them costs less than probabilities
-// that the forward pass would have to write.  32,768 x 256 of bf16 10.3 us, 3.3 TB/s
-// read and written (with 512 workgroups 15 % longer).
+// that the forward pass would have to write.  Bound by its vector instructions, 77 % of
+// a compute unit's busy cycles (the exponentials 12 %): 32,768 x 256 of bf16 10.6 us,
+// 3.2 TB/s read and written (with 512 workgroups 15 % longer).
 constexpr int BACK_THREADS = 256, BACK_WAVES = 4;
 constexpr uint32_t BACK_GROUPS = 1024;   // workgroups at most
 

@@ -205,9 +205,11 @@ __device__ inline void deal(uint32_t id, uint32_t mt, uint32_t nt, uint32_t &m, 
 // first copies and stores.  With results of 32 bits 770 us, 1.4 PFLOP/s, bound by
 // the matrix units' 16-bit rate.  EXPERTS: bound by reading the weights where an
 // expert has few rows (512 rows of 64 experts, 2048 x 2048, 41 us, 6.5 TB/s), by the
-// products where it has many (32,768 rows, 4096 x 2048, 359 us, 1.5 PFLOP/s: one
+// products where it has many (32,768 rows, 4096 x 2048, 359 us, 1.5 PFLOP/s: ten
+// rounds of tiles with 22 us of stages and 12 of first copies and stores each, and an
 // expert's last block is half empty).  GRADIENT: bound by storing (61 experts, 1000 x
-// 2040 of f32, from 12,297 rows, 144 us, 3.5 TB/s), each tile's few stages before it
+// 2040 of f32, from 12,297 rows, 147 us in a graph of such calls, 3.4 TB/s, 169 by the
+// profiler behind the other products of a step), each tile's few stages before it
 // (without the stores 105).
 // Tiles of 128 x 128 wait for their copies: 2048 x 4096 x 8192 takes 78 us, 68 without
 // the products, 52 without the copies; eight waves a tile change nothing.
@@ -711,8 +713,9 @@ inline bool large_tiles(uint64_t small, uint64_t large, bool exact)
 // How a product is made: k in `parts` of `per` blocks; few rows with steps of
 // `each` a wave.
 // As few rows, or in tiles, in us: 1 x 4096 x 4096 6.3 and 14.3, 64 x 4096 x 4096
-// 10.2 and 15.9, 64 x 16384 x 1024 8.9 and 9.2, 64 x 65536 x 2048 35.8 and 35.7.  More
-// rows than 64 leave no registers for them.
+// 10.2 and 15.9, 64 x 16384 x 1024 8.9 and 9.2, 64 x 65536 x 2048 35.8 and 35.7 (with
+// results of 32 bits 39.2 and 36.7: there it costs a little).  More rows than 64 leave
+// no registers for them.
 constexpr uint32_t FEW_ROWS = 64;
 constexpr int FEW_WAVES = 8, FEW_AHEAD = 4;   // seven steps ahead take as long as four
 // Of a part of k in tiles.  With 4, 8 and 16, in us: 512 x 512 x 8192 20.3, 17.6 and
@@ -854,7 +857,9 @@ hipError_t launch_f8_expert_gradient(const F8MatmulArgs &a, uint32_t dtype, hipS
     return by_type(dtype, [&](auto t) -> hipError_t {
         typedef decltype(t) T;
         constexpr bool EXACT = sizeof(T) == 4;
-        // large and small: 61 experts, 1000 x 2040 of f32, 151 and 161 us, of bf16 101 and 117
+        // large and small: 61 experts, 1000 x 2040 from 12,297 rows, f32 150 and 154 us, bf16
+        // 95 and 102; 64 experts, 1024 x 1024 from 4096 rows, f32 66 and 58, bf16 43 and 45 (a
+        // tile's stages, few there, are not among what the rule goes by)
         if (large_tiles(a.experts * tiles_of(a.m, a.n), a.experts * tiles_of(a.m, a.n, 256), EXACT))
             return product<T, EXACT, GRADIENT, 256, 256, 2, 2, 2>(a, (uint32_t)((a.m + 255) / 256), a.experts, 0, s);
         return product<T, EXACT, GRADIENT, 128, 128, 2, 2, 2>(a, (uint32_t)((a.m + 127) / 128), a.experts, 0, s);

@@ -437,11 +437,14 @@ class Operators:
 
     def quantize8_columns(self, x, groups: Optional[Groups] = None) -> F8:
         """x's columns (the rows of its transpose); with groups, in blocks of one
-        expert's rows, as expert_gradient8() takes them."""
+        expert's rows, as expert_gradient8() takes them.  Blocks behind the last
+        expert's are not written: they hold what the memory held."""
         return self._pack8(x, False, True, groups=groups)[1]
 
     def quantize8_both(self, x, groups: Optional[Groups] = None):
-        """(x's rows, x's columns) in one pass over x."""
+        """(x's rows, x's columns) in one pass over x.  With groups, rows that are no
+        expert's and blocks of the columns behind the last expert's are not written:
+        they hold what the memory held, and no expert's operator reads them."""
         return self._pack8(x, True, True, groups=groups)
 
     def quantize8_tiles(self, w):
@@ -484,7 +487,8 @@ class Operators:
 
     def expert_matmul8(self, a: F8, w: F8, groups: Groups, dtype, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """[rows of a, n]: each row of a, in expert order, times its expert's w
-        [experts, n, a.cols].  Rows that are no expert's are left as they were."""
+        [experts, n, a.cols].  Rows that are no expert's are left as they were:
+        without `out` they hold what the memory held."""
         kind = self._type(dtype)
         if a.cols != w.cols:
             raise ValueError(f"a has rows of {a.cols} values, w of {w.cols}")
